@@ -89,7 +89,8 @@ const char *ag_last_error(const ag_ctx *ctx);
  * compacts into the workspace) and ag_decode_attn over caches of at most `cache_rows` rows in total. */
 size_t ag_workspace_bytes(int B, int L, int Hq, int Hkv, int D, ag_dtype dtype, int d_in, int64_t cache_rows);
 
-/* Synchronise `stream`, read and clear the sticky device error word.  AG_OK or AG_ECAPACITY.
+/* Synchronise `stream`, read and clear the sticky device error word.  AG_OK, AG_ECAPACITY, or AG_EINVAL (a position outside
+ * the table of an ag_rope).
  * (Kernel timing and machine probes for benchmarks are declared in ag_bench.h; they are no part of the method.) */
 ag_status ag_poll_error(ag_ctx *ctx, void *hip_stream);
 
@@ -276,6 +277,86 @@ ag_status ag_recent_fill(ag_ctx *ctx, void *hip_stream, const void *k, const voi
 ag_status ag_decode_attn_recent(ag_ctx *ctx, void *hip_stream, const void *q, const void *k_new, const void *v_new,
                                 const uint8_t *new_flags, int pos, int Hq, float scale, ag_kv_cache *cache,
                                 ag_recent_ring *ring, void *out);
+
+/*
+ * Rotary positions.  Pair i of a vector is its values i and i + D/2; with p = pos[axis(i)][b][t] and the angle's cosine and
+ * sine from row p of `table`,
+ *   y_i = x_i cos - x_(i+D/2) sin,   y_(i+D/2) = x_(i+D/2) cos + x_i sin
+ * products and sum rounded one by one in 32 bits, then once to the vectors' type.  Pairs [0, section[0]) turn by the first
+ * axis, the next section[1] by the second, the next section[2] by the third (text: one axis, section[0] = D/2; images and
+ * video: height, width; time, height, width); the sections of the n_axes axes add up to D/2.  All pointers are device memory, the
+ * table 16-byte aligned.  A position outside [0, n_rows) is turned by the nearest row, and ag_poll_error reports AG_EINVAL.
+ */
+typedef struct {
+  const float *table;  /* [n_rows, D]: row p holds the D/2 cosines, then the D/2 sines       */
+  const int32_t *pos;  /* [n_axes, B, L]                                                     */
+  int32_t n_rows;
+  int32_t n_axes;      /* 1 to 3                                                             */
+  int32_t section[3];  /* pairs of each axis                                                 */
+} ag_rope;
+
+/*
+ * Queries and keys turned by their positions, in one launch: q, q_out [B, Hq, L, D], k, k_out [B, Hkv, L, D] in `dtype`;
+ * q_out may be q, k_out may be k.  k and k_out may be NULL (Hkv is then ignored).  bf16 or fp32, D a multiple of 16 and at most
+ * 512; all tensors 16-byte aligned.  Needs no workspace.
+ */
+ag_status ag_rotate(ag_ctx *ctx, void *hip_stream, const void *q, const void *k, ag_dtype dtype, int B, int Hq, int Hkv, int L,
+                    int D, const ag_rope *rope, void *q_out, void *k_out);
+
+/*
+ * Paged 8-bit cache.  Unit u = b * Hkv + g counts its rows in order of arrival; rows 64 j .. 64 j + 63 are its block j.
+ *   - A full block is held in 8 bits: value = code 2^e, the codes e4m3 numbers (round to nearest even), e the least integer >= -100
+ *     with max |x| 2^-e <= 448 over the block's finite values, for K and V each; what is not finite becomes NaN.  Its codes lie in page
+ *     page[u][j], which the caller has given it; scale[page] = 2^e.  Units may share pages that hold the same full blocks.
+ *   - The last, incomplete block is held in bf16 in the unit's tail; it is rounded to 8 bits when its 64th row arrives, from those bf16
+ *     numbers.  So the cache does not depend on how its rows were cut into calls.  Rows of the tail past len % 64 hold anything.
+ *   - Order of a page's 64 D codes, and of a tail's values (row t, column d), made for the matrix instructions:
+ *       K: ((t / 16 * (D / 64) + d / 64) * 4 + d / 16 % 4) * 256 + t % 16 * 16 + d % 16
+ *       V: (d / 16 * 4 + t / 4 % 4) * 256 + d % 16 * 16 + t / 16 * 4 + t % 4
+ * A unit has room up to the row that would fill a block that has no page (j >= max_blocks, or page[u][j] outside [0, n_pages));
+ * that row and those after it are dropped (ag_poll_error: AG_ECAPACITY).  A full block whose page number is outside the pool is
+ * not read: its rows count as evicted.  bf16 inputs; D = 128 or 64; Hq / Hkv in {1, 2, 4, 8}; at most 8192 units; tensors
+ * 16-byte aligned; a rope's sections multiples of 4 pairs (ag_rotate takes any), rope = NULL where q and k arrive
+ * position-encoded.
+ */
+#define AG_Q8_BLOCK 64
+
+typedef struct {
+  void *k, *v;              /* [n_pages, 64 D] codes                                     */
+  float *k_scale, *v_scale; /* [n_pages]                                                 */
+  void *k_tail, *v_tail;    /* [B*Hkv, 64 D] bf16                                        */
+  const int32_t *page;      /* [B*Hkv, max_blocks]                                       */
+  int32_t *len;             /* [B*Hkv] rows held; updated by the calls                   */
+  int32_t n_pages, max_blocks;
+  int32_t B, Hkv, D;
+} ag_q8_cache;
+
+/* Workspace that covers the calls below (L = 1: ag_q8_decode_attn) on one cache; Hq = Hkv will do for ag_q8_append alone. */
+size_t ag_q8_workspace_bytes(int B, int L, int Hq, int Hkv, int D, int max_blocks);
+
+/*
+ * The tokens t of k, v [B, Hkv, L, D] with flags[b,g,t] != 0 (flags = NULL: all) join their units in order of t, keys turned by
+ * rope->pos [n_axes, B, L].
+ */
+ag_status ag_q8_append(ag_ctx *ctx, void *hip_stream, const void *k, const void *v, const uint8_t *flags, int L,
+                       const ag_rope *rope, ag_q8_cache *cache);
+
+/*
+ * Attention of L new tokens of every sequence, then ag_q8_append of the same k, v, flags: the first prompt (empty cache) or a later
+ * turn of a conversation.  Row j of query head i (KV head g = i / (Hq/Hkv)) sees the unit's rows as the cache held them before
+ * the call, the call's tokens { t < j : flags[b,g,t] != 0 }, and j itself:
+ *   out[b,i,j,:] = sum softmax(scale * q_j . k) v     (fp32 accumulate; q and k turned)
+ * q, out [B, Hq, L, D].  A token that sees nothing else gets out[j] = v[j]; kept tokens that found no room count as evicted.
+ */
+ag_status ag_q8_prefill_attn(ag_ctx *ctx, void *hip_stream, const void *q, const void *k, const void *v, const uint8_t *flags,
+                             int L, int Hq, const ag_rope *rope, float scale, ag_q8_cache *cache, void *out);
+
+/*
+ * One decoding step: the same with L = 1, in one launch.  q, out [B, Hq, D]; k_new, v_new [B, Hkv, D]; new_flags uint8 [B, Hkv] or
+ * NULL; rope->pos [n_axes, B, 1].
+ */
+ag_status ag_q8_decode_attn(ag_ctx *ctx, void *hip_stream, const void *q, const void *k_new, const void *v_new,
+                            const uint8_t *new_flags, int Hq, const ag_rope *rope, float scale, ag_q8_cache *cache, void *out);
 
 #ifdef __cplusplus
 }

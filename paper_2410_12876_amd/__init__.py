@@ -27,7 +27,8 @@ STATUS_NAMES = ["AG_OK", "AG_EINVAL", "AG_EUNSUPPORTED", "AG_ECAPACITY", "AG_EWO
 EXPORTS = ["ag_create", "ag_destroy", "ag_last_error", "ag_workspace_bytes", "ag_poll_error",
            "ag_timing_kernels", "ag_timing_kernel_name", "ag_timing_enable", "ag_timing_read",
            "ag_probe_mfma", "ag_probe_mfma_data", "ag_probe_mfma_duty", "ag_probe_copy", "ag_probe_projection_tile", "ag_gate", "ag_rmsnorm_gate", "ag_compact_kv", "ag_pack_row_off", "ag_prefill_attn", "ag_prefill_attn_recent",
-           "ag_compact_prefill_attn", "ag_project_compact_kv", "ag_project_compact_workspace_bytes", "ag_decode_attn", "ag_decode_attn_static", "ag_decode_static_scratch_bytes", "ag_decode_scratch_bytes", "ag_recent_fill", "ag_decode_attn_recent", "ag_gate_mha", "ag_gate_mha_workspace_bytes"]
+           "ag_compact_prefill_attn", "ag_project_compact_kv", "ag_project_compact_workspace_bytes", "ag_decode_attn", "ag_decode_attn_static", "ag_decode_static_scratch_bytes", "ag_decode_scratch_bytes", "ag_recent_fill", "ag_decode_attn_recent", "ag_gate_mha", "ag_gate_mha_workspace_bytes",
+           "ag_rotate", "ag_q8_workspace_bytes", "ag_q8_append", "ag_q8_prefill_attn", "ag_q8_decode_attn"]
 
 
 class ag_recent_ring(C.Structure):
@@ -45,6 +46,16 @@ class ag_kv_cache(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("idx", C.c_void_p), ("row_off", C.c_void_p),
                 ("len", C.c_void_p), ("total_rows", C.c_int64), ("B", C.c_int32), ("Hkv", C.c_int32),
                 ("D", C.c_int32), ("dtype", C.c_int)]
+
+
+class ag_rope(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("pos", C.c_void_p), ("n_rows", C.c_int32), ("n_axes", C.c_int32), ("section", C.c_int32 * 3)]
+
+
+class ag_q8_cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("k_tail", C.c_void_p), ("v_tail", C.c_void_p), ("page", C.c_void_p), ("len", C.c_void_p),
+                ("n_pages", C.c_int32), ("max_blocks", C.c_int32), ("B", C.c_int32), ("Hkv", C.c_int32), ("D", C.c_int32)]
 
 
 _lib = None
@@ -126,6 +137,16 @@ def load() -> C.CDLL:
     lib.ag_decode_attn_recent.restype = C.c_int
     lib.ag_decode_attn_recent.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, f32, C.POINTER(ag_kv_cache),
                                           C.POINTER(ag_recent_ring), vp]
+    lib.ag_rotate.restype = C.c_int
+    lib.ag_rotate.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, C.POINTER(ag_rope), vp, vp]
+    lib.ag_q8_workspace_bytes.restype = C.c_size_t
+    lib.ag_q8_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32]
+    lib.ag_q8_append.restype = C.c_int
+    lib.ag_q8_append.argtypes = [vp, vp, vp, vp, vp, i32, C.POINTER(ag_rope), C.POINTER(ag_q8_cache)]
+    lib.ag_q8_prefill_attn.restype = C.c_int
+    lib.ag_q8_prefill_attn.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, C.POINTER(ag_rope), f32, C.POINTER(ag_q8_cache), vp]
+    lib.ag_q8_decode_attn.restype = C.c_int
+    lib.ag_q8_decode_attn.argtypes = [vp, vp, vp, vp, vp, vp, i32, C.POINTER(ag_rope), f32, C.POINTER(ag_q8_cache), vp]
     import torch  # noqa: F401  (the binding module uses its libraries)
     from . import _binding
     _lib, _native = lib, _binding
@@ -351,3 +372,74 @@ def ag_gate_mha(ctx: Context, x, w_qkv, h_prime: int, d_prime: int, w_o, bias, t
     bias f32 [H_f]; logits_out f32 [B, L, H_f] or None; flags_out u8 [B, H_f, L]."""
     ctx._check(ctx._native.gate_mha(ctx._addr, stream, x, w_qkv, h_prime, d_prime, w_o, bias, tau, n_sink,
                                     logits_out, flags_out))
+
+Q8_BLOCK = 64  # rows of a block of the paged 8-bit cache
+
+
+class Rope:
+    """ag_rope over caller-made device tensors: table f32 [n_rows, D] (D/2 cosines, then D/2 sines of a row's angles), pos i32
+    [n_axes, B, L]; section: pairs that turn by each axis (None: all by the only one)."""
+
+    def __init__(self, table, pos, section=None):
+        import torch
+        if table.dim() != 2 or table.dtype != torch.float32:
+            raise ValueError("the table is fp32 [n_rows, D]")
+        if pos.dim() != 3 or pos.dtype != torch.int32:
+            raise ValueError("pos is int32 [n_axes, B, L]")
+        section = [table.shape[1] // 2] if section is None else list(section)
+        if len(section) != pos.shape[0] or len(section) > 3:
+            raise ValueError("pos has %d axes, section %d (at most 3)" % (pos.shape[0], len(section)))
+        self.table, self.pos, self.section = table, pos, section
+        self.c = ag_rope(_ptr(table), _ptr(pos), table.shape[0], len(section), (C.c_int32 * 3)(*section))
+
+    def _of(self, D: int, B: int, L: int):
+        """The structure, for vectors of D values of B sequences of L tokens."""
+        if self.table.shape[1] != D or self.pos.shape[1] != B or self.pos.shape[2] != L:
+            raise ValueError("table %s, pos %s: not for vectors of %d, %d sequences of %d tokens" %
+                             (tuple(self.table.shape), tuple(self.pos.shape), D, B, L))
+        return self.c
+
+
+class Q8Cache:
+    """ag_q8_cache over caller-made device tensors: k, v u8 (or 8-bit float) [n_pages, 64 D]; k_scale, v_scale f32 [n_pages];
+    k_tail, v_tail bf16 [B*Hkv, 64 D]; page i32 [B*Hkv, max_blocks] (the page of each block, -1: none yet); len i32 [B*Hkv]."""
+
+    def __init__(self, k, v, k_scale, v_scale, k_tail, v_tail, page, len_, B: int, Hkv: int, D: int):
+        import torch
+        U, n = B * Hkv, k.shape[0]
+        for t, shape, dtype in ((k, (n, Q8_BLOCK * D), None), (v, (n, Q8_BLOCK * D), None), (k_scale, (n,), torch.float32),
+                                (v_scale, (n,), torch.float32), (k_tail, (U, Q8_BLOCK * D), torch.bfloat16),
+                                (v_tail, (U, Q8_BLOCK * D), torch.bfloat16), (page, (U, page.shape[-1]), torch.int32), (len_, (U,), torch.int32)):
+            if tuple(t.shape) != shape or (t.dtype != dtype if dtype else t.element_size() != 1):
+                raise ValueError("a tensor of the cache is %s %s, not %s %s" % (t.dtype, tuple(t.shape), dtype or "8 bits", shape))
+        self.k, self.v, self.k_scale, self.v_scale, self.k_tail, self.v_tail, self.page, self.len = k, v, k_scale, v_scale, k_tail, v_tail, page, len_
+        self.B, self.Hkv, self.D = B, Hkv, D
+        self.c = ag_q8_cache(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(k_tail), _ptr(v_tail), _ptr(page), _ptr(len_), n,
+                             int(page.shape[1]), B, Hkv, D)
+
+
+def q8_workspace_bytes(B: int, L: int, Hq: int, Hkv: int, D: int, max_blocks: int) -> int:
+    return int(load().ag_q8_workspace_bytes(B, L, Hq, Hkv, D, max_blocks))
+
+
+def ag_rotate(ctx: Context, q, k, rope: Rope, q_out, k_out, stream=None) -> None:
+    """q, q_out [B, Hq, L, D], k, k_out [B, Hkv, L, D] (or None): turned by rope.pos [n_axes, B, L]; q_out may be q, k_out may be k."""
+    ctx._check(ctx._native.rotate(ctx._addr, stream, q, k, rope._of(q.shape[-1], q.shape[0], q.shape[2]), q_out, k_out))
+
+
+def ag_q8_append(ctx: Context, k, v, flags, rope: Optional[Rope], cache: Q8Cache, stream=None) -> None:
+    """k, v [B, Hkv, L, D] bf16, flags u8 [B, Hkv, L] or None (all): the kept tokens join the cache, keys turned by rope."""
+    ctx._check(ctx._native.q8_append(ctx._addr, stream, k, v, flags, rope._of(cache.D, cache.B, k.shape[2]) if rope is not None else None, cache.c))
+
+
+def ag_q8_prefill_attn(ctx: Context, q, k, v, flags, rope: Optional[Rope], scale: float, cache: Q8Cache, out, stream=None) -> None:
+    """q, out [B, Hq, L, D]; k, v [B, Hkv, L, D]; flags u8 [B, Hkv, L] or None: attention over the cache as it stands and over the
+    call's own kept tokens, then ag_q8_append."""
+    ctx._check(ctx._native.q8_prefill_attn(ctx._addr, stream, q, k, v, flags, rope._of(cache.D, cache.B, q.shape[2]) if rope is not None else None,
+                                           scale, cache.c, out))
+
+
+def ag_q8_decode_attn(ctx: Context, q, k_new, v_new, new_flags, rope: Optional[Rope], scale: float, cache: Q8Cache, out, stream=None) -> None:
+    """q, out [B, Hq, D]; k_new, v_new [B, Hkv, D]; new_flags u8 [B, Hkv] or None; rope.pos [n_axes, B, 1]; cache updated in place."""
+    ctx._check(ctx._native.q8_decode_attn(ctx._addr, stream, q, k_new, v_new, new_flags, rope._of(cache.D, cache.B, 1) if rope is not None else None,
+                                          scale, cache.c, out))

@@ -22,19 +22,6 @@ ag_status ag_fail(ag_ctx *ctx, ag_status st, const char *fmt, ...) {
 
 namespace {
 
-constexpr int kMaxL = 1 << 22;
-
-#define AG_REQUIRE(cond, st, ...) \
-  do {                            \
-    if (!(cond)) return ag_fail(ctx, st, __VA_ARGS__); \
-  } while (0)
-
-#define AG_HIP(call)                                                                   \
-  do {                                                                                 \
-    hipError_t e_ = (call);                                                            \
-    if (e_ != hipSuccess) return ag_fail(ctx, AG_EHIP, "%s: %s", #call, hipGetErrorString(e_)); \
-  } while (0)
-
 bool dtype_ok(int dt) { return dt == AG_F32 || dt == AG_BF16; }
 
 ag_status check_cache(ag_ctx *ctx, const ag_kv_cache *c) {
@@ -48,14 +35,14 @@ ag_status check_cache(ag_ctx *ctx, const ag_kv_cache *c) {
 
 ws_cursor cursor(ag_ctx *ctx) { return ws_cursor{ctx->ws, ctx->ws_bytes, 0, true}; }
 
-ag_status need_device(ag_ctx *ctx) {
+}  // namespace
+
+ag_status ag_need_device(ag_ctx *ctx) {
   if (ctx->device < 0) return ag_fail(ctx, AG_EHIP, "context has no device (created with device = -1)");
   hipError_t e = hipSetDevice(ctx->device);
   if (e != hipSuccess) return ag_fail(ctx, AG_EHIP, "hipSetDevice(%d): %s", ctx->device, hipGetErrorString(e));
   return AG_OK;
 }
-
-}  // namespace
 
 constexpr size_t kTailBytes = 256 + (kDecodeMaxUnits + kDecodeArriveInts + kPrefillTickets) * sizeof(int32_t);
 
@@ -121,7 +108,8 @@ void ag_destroy(ag_ctx *ctx) {
 
 static const char *const kKernelNames[AG_K_COUNT] = {"gate", "gate_finalize", "flag_scan", "compact",
                                                      "prefill", "decode_partial", "decode_merge",
-                                                     "mha_proj", "mha_attn", "norm_gate"};
+                                                     "mha_proj", "mha_attn", "norm_gate", "rotate", "q8_fill",
+                                                     "q8_prefill", "q8_decode"};
 
 int ag_timing_kernels(void) { return AG_K_COUNT; }
 
@@ -131,7 +119,7 @@ const char *ag_timing_kernel_name(int kernel_id) {
 
 ag_status ag_timing_enable(ag_ctx *ctx, int on) {
   if (!ctx) return AG_EINVAL;
-  ag_status st = need_device(ctx);
+  ag_status st = ag_need_device(ctx);
   if (st != AG_OK) return st;
   if (on) {
     for (int id = 0; id < AG_K_COUNT; ++id) {
@@ -156,7 +144,7 @@ ag_status ag_timing_read(ag_ctx *ctx, int kernel_id, double *total_ms, int *laun
   if (!ctx) return AG_EINVAL;
   AG_REQUIRE(kernel_id >= 0 && kernel_id < AG_K_COUNT && total_ms && launches, AG_EINVAL,
              "ag_timing_read: bad kernel id or null pointer");
-  ag_status st = need_device(ctx);
+  ag_status st = ag_need_device(ctx);
   if (st != AG_OK) return st;
   const ag_timer &t = ctx->timers[kernel_id];
   double sum = 0.0;
@@ -202,7 +190,7 @@ size_t ag_workspace_bytes(int B, int L, int Hq, int Hkv, int D, ag_dtype dtype, 
 
 ag_status ag_poll_error(ag_ctx *ctx, void *hip_stream) {
   if (!ctx) return AG_EINVAL;
-  ag_status st = need_device(ctx);
+  ag_status st = ag_need_device(ctx);
   if (st != AG_OK) return st;
   int32_t h = 0;
   AG_HIP(hipMemcpyAsync(&h, ctx->d_err, sizeof(h), hipMemcpyDeviceToHost, (hipStream_t)hip_stream));
@@ -210,7 +198,8 @@ ag_status ag_poll_error(ag_ctx *ctx, void *hip_stream) {
   if (h) {
     AG_HIP(hipMemsetAsync(ctx->d_err, 0, sizeof(h), (hipStream_t)hip_stream));
     AG_HIP(hipStreamSynchronize((hipStream_t)hip_stream));
-    return ag_fail(ctx, AG_ECAPACITY, "a cache unit overflowed its capacity; the extra rows were dropped");
+    if (h & 1) return ag_fail(ctx, AG_ECAPACITY, "a cache unit overflowed its capacity; the extra rows were dropped");
+    return ag_fail(ctx, AG_EINVAL, "a position lies outside the rotation table; the nearest row was used");
   }
   return AG_OK;
 }
@@ -229,7 +218,7 @@ ag_status ag_gate(ag_ctx *ctx, void *hip_stream, const void *feat, ag_dtype dtyp
   AG_REQUIRE(dtype != AG_BF16 || d_in % 64 == 0, AG_EUNSUPPORTED, "ag_gate: bf16 needs d_in %% 64 == 0 (got %d)", d_in);
   AG_REQUIRE(ag_ws_gate_bytes((int64_t)B * L, d_in, H_f, dtype) <= ctx->ws_bytes, AG_EWORKSPACE,
              "ag_gate: workspace of %zu bytes is too small", ctx->ws_bytes);
-  ag_status st = need_device(ctx);
+  ag_status st = ag_need_device(ctx);
   if (st != AG_OK) return st;
   const float thr = (float)log((double)tau / (1.0 - (double)tau));
   ws_cursor ws = cursor(ctx);
@@ -259,7 +248,7 @@ ag_status ag_rmsnorm_gate(ag_ctx *ctx, void *hip_stream, const void *h, ag_dtype
              "ag_rmsnorm_gate: h, x_out and norm_w must be 16-byte aligned");
   AG_REQUIRE(ag_ws_gate_bytes((int64_t)B * L, d_in, H_f, dtype) <= ctx->ws_bytes, AG_EWORKSPACE,
              "ag_rmsnorm_gate: workspace of %zu bytes is too small", ctx->ws_bytes);
-  ag_status st = need_device(ctx);
+  ag_status st = ag_need_device(ctx);
   if (st != AG_OK) return st;
   const float thr = (float)log((double)tau / (1.0 - (double)tau));
   ws_cursor ws = cursor(ctx);
@@ -293,7 +282,7 @@ ag_status ag_gate_mha(ag_ctx *ctx, void *hip_stream, const void *x, ag_dtype dty
   AG_REQUIRE((int64_t)B * h_prime <= 65535 && (int64_t)d_model * 3 * h_prime * 128 < (1ll << 30) &&
                  (int64_t)B * L < (1ll << 31) - 128,
              AG_EUNSUPPORTED, "ag_gate_mha: problem too large");
-  ag_status st = need_device(ctx);
+  ag_status st = ag_need_device(ctx);
   if (st != AG_OK) return st;
   const float thr = (float)log((double)tau / (1.0 - (double)tau));
   ws_cursor ws = cursor(ctx);
@@ -315,7 +304,7 @@ ag_status ag_compact_kv(ag_ctx *ctx, void *hip_stream, const void *k, const void
   const int units = cache->B * cache->Hkv;
   AG_REQUIRE(ag_ws_scan_bytes(units, L) <= ctx->ws_bytes, AG_EWORKSPACE,
              "ag_compact_kv: workspace of %zu bytes is too small", ctx->ws_bytes);
-  st = need_device(ctx);
+  st = ag_need_device(ctx);
   if (st != AG_OK) return st;
   const int nw = ag_nwords(L);
   ws_cursor ws = cursor(ctx);
@@ -341,7 +330,7 @@ ag_status ag_pack_row_off(ag_ctx *ctx, void *hip_stream, const uint8_t *flags, i
   ws_cursor ws = cursor(ctx);
   int32_t *kept = ws.take<int32_t>(units);
   AG_REQUIRE(ws.ok, AG_EWORKSPACE, "ag_pack_row_off: workspace of %zu bytes is too small (need %zu)", ctx->ws_bytes, ws.off);
-  ag_status st = need_device(ctx);
+  ag_status st = ag_need_device(ctx);
   if (st != AG_OK) return st;
   AG_HIP(ag_launch_pack_row_off(ctx, (hipStream_t)hip_stream, flags, units, L, room, total_rows, kept, row_off, rows_needed));
   return AG_OK;
@@ -370,7 +359,7 @@ ag_status ag_project_compact_kv(ag_ctx *ctx, void *hip_stream, const void *x, ag
   const int units = B * cache->Hkv;
   AG_REQUIRE(ag_ws_project_compact_bytes(units, L) <= ctx->ws_bytes, AG_EWORKSPACE,
              "ag_project_compact_kv: workspace of %zu bytes is too small", ctx->ws_bytes);
-  st = need_device(ctx);
+  st = ag_need_device(ctx);
   if (st != AG_OK) return st;
   ws_cursor ws = cursor(ctx);
   hipError_t e = ag_launch_project_compact(ctx, (hipStream_t)hip_stream, x, B, L, d_model, w_kv, cache->Hkv, flags, pos0,
@@ -440,7 +429,7 @@ ag_status prefill_common(ag_ctx *ctx, void *hip_stream, const void *q, const voi
   if (tuned) ag_prefill_bf16_plan(ctx->num_cu, B, L, Hq, Hkv, D, ws, &plan, &part);
   AG_REQUIRE(ws.ok, AG_EWORKSPACE, "ag_prefill_attn: workspace of %zu bytes is too small (need %zu)", ctx->ws_bytes,
              ws.off);
-  ag_status st = need_device(ctx);
+  ag_status st = ag_need_device(ctx);
   if (st != AG_OK) return st;
   hipStream_t s = (hipStream_t)hip_stream;
   const ag_pf_plan *pl = tuned ? &plan : nullptr;
@@ -494,7 +483,7 @@ ag_status ag_recent_fill(ag_ctx *ctx, void *hip_stream, const void *k, const voi
   AG_REQUIRE(dtype_ok(dtype), AG_EINVAL, "ag_recent_fill: unknown dtype %d", (int)dtype);
   ag_status st = check_ring(ctx, ring);
   if (st != AG_OK) return st;
-  st = need_device(ctx);
+  st = ag_need_device(ctx);
   if (st != AG_OK) return st;
   AG_HIP(ag_launch_ring_fill((hipStream_t)hip_stream, k, v, flags, B * Hkv, L, D, dtype, pos0, ring_dev(ring)));
   return AG_OK;
@@ -565,7 +554,7 @@ ag_status decode_common(ag_ctx *ctx, void *hip_stream, const void *q, const void
   else
     AG_REQUIRE(need <= ctx->ws_bytes, AG_EWORKSPACE, "ag_decode_attn: workspace of %zu bytes is too small",
                ctx->ws_bytes);
-  st = need_device(ctx);
+  st = ag_need_device(ctx);
   if (st != AG_OK) return st;
   ws_cursor ws = static_scratch ? ws_cursor{ctx->static_scratch, kStaticScratchBytes, 0, true} : cursor(ctx);
   hipError_t e = ag_launch_decode(ctx, (hipStream_t)hip_stream, q, k_new, v_new, new_flags, pos, cache->B, Hq, cache->Hkv,

@@ -254,10 +254,88 @@ AG_BINDING(gate_mha, 10) {
   return call([&] { return ag_gate_mha(ctx, s, xp, dt, B, L, d, w, hp, dp, wop, bias, H, tau, n_sink, logits, flags); });
 }
 
+// q, k, rope, q_out, k_out
+AG_BINDING(rotate, 5) {
+  const at::Tensor &q = tensor(a[0]);
+  const int B = dim(q, 4, 0), Hq = dim(q, 4, 1), L = dim(q, 4, 2), D = dim(q, 4, 3);
+  int Hkv = 0;
+  if (a[1] != Py_None) {
+    const at::Tensor &k = tensor(a[1]);
+    Hkv = dim(k, 4, 1);
+    if (k.scalar_type() != q.scalar_type() || k.size(0) != B || k.size(2) != L || k.size(3) != D)
+      fail(PyExc_ValueError, "rotate: q and k differ in more than their heads");
+  }
+  const ag_dtype dt = dtype_of(q);
+  const void *qp = ptr(a[0]), *k = ptr(a[1]);
+  const ag_rope *r = struct_of<ag_rope>(a[2]);
+  void *qo = ptr(a[3]), *ko = ptr(a[4]);
+  return call([&] { return ag_rotate(ctx, s, qp, k, dt, B, Hq, Hkv, L, D, r, qo, ko); });
+}
+
+// The shape of a call's tensors against the cache's: [B, Hkv, (L,) D] in bf16.
+void like_cache(const at::Tensor &t, const ag_q8_cache *c, int dims) {
+  if (t.scalar_type() != at::kBFloat16) fail(PyExc_ValueError, "the paged 8-bit cache takes bf16 tensors");
+  if (c && (dim(t, dims, 0) != c->B || t.size(1) != c->Hkv || t.size(dims - 1) != c->D))
+    fail(PyExc_ValueError, "a tensor's shape differs from the cache's");
+}
+void like(const at::Tensor &t, const at::Tensor &other, const char *msg) {
+  if (t.scalar_type() != other.scalar_type() || t.sizes() != other.sizes()) fail(PyExc_ValueError, msg);
+}
+
+// k, v, flags, rope, cache
+AG_BINDING(q8_append, 5) {
+  const at::Tensor &k = tensor(a[0]);
+  const int L = dim(k, 4, 2);
+  const ag_rope *r = struct_of<ag_rope>(a[3]);
+  ag_q8_cache *c = struct_of<ag_q8_cache>(a[4]);
+  like_cache(k, c, 4);
+  like(tensor(a[1]), k, "k and v differ");
+  const void *kp = ptr(a[0]), *v = ptr(a[1]);
+  const uint8_t *f = ptr_as<uint8_t>(a[2]);
+  return call([&] { return ag_q8_append(ctx, s, kp, v, f, L, r, c); });
+}
+
+// q, k, v, flags, rope, scale, cache, out
+AG_BINDING(q8_prefill_attn, 8) {
+  const at::Tensor &q = tensor(a[0]), &k = tensor(a[1]);
+  const int Hq = dim(q, 4, 1), L = dim(q, 4, 2);
+  const ag_rope *r = struct_of<ag_rope>(a[4]);
+  const float scale = float_of(a[5]);
+  ag_q8_cache *c = struct_of<ag_q8_cache>(a[6]);
+  like_cache(k, c, 4);
+  like(tensor(a[2]), k, "k and v differ");
+  like(tensor(a[7]), q, "out and q differ");
+  if (q.scalar_type() != k.scalar_type() || q.size(0) != k.size(0) || k.size(2) != L || q.size(3) != k.size(3))
+    fail(PyExc_ValueError, "q and k differ in more than their heads");
+  const void *qp = ptr(a[0]), *kp = ptr(a[1]), *v = ptr(a[2]);
+  const uint8_t *f = ptr_as<uint8_t>(a[3]);
+  void *out = ptr(a[7]);
+  return call([&] { return ag_q8_prefill_attn(ctx, s, qp, kp, v, f, L, Hq, r, scale, c, out); });
+}
+
+// q, k_new, v_new, new_flags, rope, scale, cache, out
+AG_BINDING(q8_decode_attn, 8) {
+  const at::Tensor &q = tensor(a[0]), &k = tensor(a[1]);
+  const int Hq = dim(q, 3, 1);
+  const ag_rope *r = struct_of<ag_rope>(a[4]);
+  const float scale = float_of(a[5]);
+  ag_q8_cache *c = struct_of<ag_q8_cache>(a[6]);
+  like_cache(k, c, 3);
+  like(tensor(a[2]), k, "k_new and v_new differ");
+  like(tensor(a[7]), q, "out and q differ");
+  if (q.scalar_type() != k.scalar_type() || q.size(0) != k.size(0) || q.size(2) != k.size(2))
+    fail(PyExc_ValueError, "q and k_new differ in more than their heads");
+  const void *qp = ptr(a[0]), *kp = ptr(a[1]), *v = ptr(a[2]);
+  const uint8_t *f = ptr_as<uint8_t>(a[3]);
+  void *out = ptr(a[7]);
+  return call([&] { return ag_q8_decode_attn(ctx, s, qp, kp, v, f, Hq, r, scale, c, out); });
+}
+
 #define AG_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {AG_METHOD(gate), AG_METHOD(rmsnorm_gate), AG_METHOD(compact_kv), AG_METHOD(pack_row_off),
                          AG_METHOD(project_compact_kv), AG_METHOD(prefill_attn), AG_METHOD(compact_prefill_attn),
                          AG_METHOD(decode_attn), AG_METHOD(decode_attn_static), AG_METHOD(recent_fill), AG_METHOD(gate_mha),
+                         AG_METHOD(rotate), AG_METHOD(q8_append), AG_METHOD(q8_prefill_attn), AG_METHOD(q8_decode_attn),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "Calls into libag on torch tensors.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};

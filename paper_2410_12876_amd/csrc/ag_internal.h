@@ -10,7 +10,8 @@
 
 // Kernels that ag_timing_* can time (ids are part of the ABI, see ag_bench.h).
 enum { AG_K_GATE = 0, AG_K_GATE_FINALIZE, AG_K_FLAG_SCAN, AG_K_COMPACT, AG_K_PREFILL, AG_K_DECODE_PARTIAL,
-       AG_K_DECODE_MERGE, AG_K_MHA_PROJ, AG_K_MHA_ATTN, AG_K_NORM_GATE, AG_K_COUNT };
+       AG_K_DECODE_MERGE, AG_K_MHA_PROJ, AG_K_MHA_ATTN, AG_K_NORM_GATE, AG_K_ROTATE, AG_K_Q8_FILL, AG_K_Q8_PREFILL,
+       AG_K_Q8_DECODE, AG_K_COUNT };
 constexpr int kTimerSlots = 1024;  // launches remembered per kernel id
 constexpr int kDecodeMaxUnits = 8192;  // (batch, KV head) units of one decode step
 constexpr int kDecodeArriveGroups = 16, kDecodeArriveStride = 64;  // counters of a step's workgroups, 256 bytes apart
@@ -28,7 +29,7 @@ struct ag_ctx {
   int num_cu;
   char *ws;         // device workspace
   size_t ws_bytes;
-  int32_t *d_err;   // sticky device error word (bit 0: cache capacity overflow)
+  int32_t *d_err;   // sticky device error word (bit 0: cache capacity overflow, bit 1: position outside a rotation table)
   int32_t *decode_tickets;  // [kDecodeMaxUnits + kDecodeArriveInts] arrival counters of a decode step: zero between launches
   int32_t *prefill_tickets; // [kPrefillTickets] arrival counters of a prefill launch without a flag scan: zero between launches
   char *static_scratch;   // this device's copy of the library's static scratch array (ag_decode_attn_static)
@@ -115,6 +116,20 @@ static inline size_t ag_align256(size_t b) { return (b + 255) & ~size_t(255); }
 static inline size_t ag_dtype_size(ag_dtype t) { return t == AG_BF16 ? 2 : 4; }
 
 ag_status ag_fail(ag_ctx *ctx, ag_status st, const char *fmt, ...);
+ag_status ag_need_device(ag_ctx *ctx);  // makes the context's device current; AG_EHIP for a context without one
+
+#define AG_REQUIRE(cond, st, ...) \
+  do {                            \
+    if (!(cond)) return ag_fail(ctx, st, __VA_ARGS__); \
+  } while (0)
+
+#define AG_HIP(call)                                                                   \
+  do {                                                                                 \
+    hipError_t e_ = (call);                                                            \
+    if (e_ != hipSuccess) return ag_fail(ctx, AG_EHIP, "%s: %s", #call, hipGetErrorString(e_)); \
+  } while (0)
+
+constexpr int kMaxL = 1 << 22;  // tokens of a call
 
 // ---- sizes of the per-call workspace blocks (host helpers, also used by ag_workspace_bytes) ----
 static inline int ag_nwords(int L) { return (L + 63) / 64; }

@@ -1,0 +1,661 @@
+// One decoding step over the paged 8-bit cache, in one launch: attention of every sequence's new token over the rows its units hold
+// and itself, and its append (q and the new key turned on the way).
+//
+// A step reads every page it attends to once: large steps are bound by HBM, small ones by dependent round trips.  The kernel builds
+// its own work list from len[] and hands data between workgroups only where a unit is too long for one.
+//   * Work is counted in items of one unit: its pages, and one for the tail and the new token.  A wave takes every NW-th item of its
+//     workgroup's segment.
+//   * A page holds 64 rows in the order of the matrix operands, so its 16-byte pieces go from memory into registers and there, widened
+//     to bf16 (exact, two values an instruction), into S^T = K q^T and O^T = V^T p^T on v_mfma_f32_16x16x32_bf16: no LDS, no barrier.  The next
+//     page's K is requested as soon as this one's is used up, its V likewise, so 8 to 16 KiB per wave are always in flight.
+//   * The 16 columns of a product are the G query heads of the group, several times: columns x and x + P (P = 4 or 8) have the same
+//     scores and carry the same weight's parts, P = 4: three bf16 numbers whose sum it is (24 bits), P = 8: two (16 bits).  That the columns
+//     would be idle otherwise makes the parts free.
+//   * The tail is a page in bf16; the new token's row is put into it in registers, so that it is one row more.  The wave that has it also
+//     stores that row, or, if it is the block's last, the whole block in 8 bits.
+//   * Segments: if the whole step gives every workgroup at most one piece of a unit (a few rounds of its waves), those; if there are more
+//     units than workgroups and all are short, one, two or four waves a unit; else all items end to end, in equal ranges.
+#include <algorithm>
+#include <type_traits>
+
+#include "ag_q8.h"
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int NW = 8, NT = 64 * NW;
+constexpr int kArriveSplit = 64;  // workgroups from which their arrivals are counted at several addresses
+constexpr int kTeamRounds = 6;    // items of a wave up to which units are given to teams of waves
+
+struct dec_args {
+  const uint16_t *q, *k_new, *v_new;
+  const uint8_t *new_flags;
+  uint16_t *out;
+  ag_q8_dev c;
+  ag_rope_dev rope;
+  float *rec;        // records [id][G][D + 2]
+  int32_t *tickets;  // [U] pieces of a unit that have stored their record; zero between launches
+  int32_t *arrived;  // workgroups that have read len[]; zero between launches
+  int32_t *err;
+  int U, Hkv;
+  float qscale;
+};
+
+__device__ __forceinline__ void put_pair(float *p, float a, float b) {
+  __hip_atomic_store(reinterpret_cast<uint64_t *>(p), (uint64_t)__float_as_uint(a) | ((uint64_t)__float_as_uint(b) << 32),
+                     __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+}
+__device__ __forceinline__ float2 get_pair(const float *p) {
+  const uint64_t x = __hip_atomic_load(reinterpret_cast<const uint64_t *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+  return make_float2(__uint_as_float((uint32_t)x), __uint_as_float((uint32_t)(x >> 32)));
+}
+__device__ __forceinline__ int wave_prefix(int x, int &total) {
+  int y = x;
+  y += __builtin_amdgcn_update_dpp(0, y, 0x111, 0xf, 0xf, false);
+  y += __builtin_amdgcn_update_dpp(0, y, 0x112, 0xf, 0xf, false);
+  y += __builtin_amdgcn_update_dpp(0, y, 0x114, 0xf, 0xf, false);
+  y += __builtin_amdgcn_update_dpp(0, y, 0x118, 0xf, 0xf, false);
+  y += __builtin_amdgcn_update_dpp(0, y, 0x142, 0xa, 0xf, false);
+  y += __builtin_amdgcn_update_dpp(0, y, 0x143, 0xc, 0xf, false);
+  total = __builtin_amdgcn_readlane(y, 63);
+  return y - x;
+}
+// Over the four lanes that share lane % 16
+__device__ __forceinline__ float kg_max(float x) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float kg_sum(float x) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+// x of the lane N columns further (of 16, cyclic)
+template <int N> __device__ __forceinline__ float column(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 + (16 - N), 0xf, 0xf, false));
+}
+
+template <int D, int G> struct wave_q8 {
+  static constexpr int KC = D / 64, KF = 4 * KC, VF = D / 16;
+  static constexpr int P = G <= 4 ? 4 : 8, PARTS = P == 4 ? 3 : 2;
+  static constexpr int SF = D + 4;  // floats per head of the state a wave leaves: max, sum, -, -, o
+  q8_bf16x8 qf[KC][2][2];
+  q8_f32x4 o[VF];
+  float m, l;
+  int lane, g, col, head, part;
+
+  __device__ __forceinline__ void init(int lane_) {
+    lane = lane_; g = lane >> 4; col = lane & 15; head = col % P; part = col / P;
+    m = kQ8EmptyMax; l = 0.f;
+#pragma unroll
+    for (int f = 0; f < VF; ++f) o[f] = q8_f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  // This lane's 16 values of each 64 columns of a vector, turned by the token's angles (in LDS: cosines, sines).
+  __device__ __forceinline__ void vector(q8_eight (&y)[KC][2], const uint16_t *x, const float *angles) {
+    uint4 raw[KC][2];
+#pragma unroll
+    for (int c = 0; c < KC; ++c)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        raw[c][s] = *reinterpret_cast<const uint4 *>(x + 64 * c + 16 * g + 8 * s);
+        y[c][s] = q8_floats(raw[c][s]);
+      }
+    if (angles) {
+#pragma unroll
+      for (int c = 0; c < KC; ++c)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          uint4 p;
+          if constexpr (KC == 2) p = raw[c ^ 1][s];
+          else p = *reinterpret_cast<const uint4 *>(x + ((16 * g + 8 * s) ^ (D / 2)));
+          y[c][s] = q8_turn8<D>(
+              [&](int i) { return q8_angles{*reinterpret_cast<const float4 *>(angles + i), *reinterpret_cast<const float4 *>(angles + D / 2 + i)}; },
+              64 * c + 16 * g + 8 * s, raw[c][s], p);
+        }
+    }
+  }
+  // The query as two bf16 numbers a value: a turned one rounded to the first alone would shift the scores by 2^-9 of their size.
+  __device__ __forceinline__ void query(const uint16_t *q, const float *angles) {
+    q8_eight y[KC][2];
+    vector(y, q + (size_t)min(head, G - 1) * D, angles);
+#pragma unroll
+    for (int c = 0; c < KC; ++c)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const uint4 hi = y[c][s].bf16();
+        const q8_eight h = q8_floats(hi);
+        qf[c][s][0] = __builtin_bit_cast(q8_bf16x8, hi);
+        qf[c][s][1] = __builtin_bit_cast(q8_bf16x8, q8_eight{y[c][s].a - h.a, y[c][s].b - h.b}.bf16());
+      }
+  }
+  // Scores of 16 rows with 32 columns of each step: sums of the two parts apart, and added at the end.
+  __device__ __forceinline__ void score(q8_f32x4 (&x)[2], int c, int h, const q8_bf16x8 &k) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) x[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qf[c][h][i], x[i], 0, 0, 0);
+  }
+  // The weights of 64 rows from their scores (score(a): rows 16 a + 4 g + 0..3), then O += p V (value(f, i): columns 16 f .., rows 32 i ..).
+  template <typename VAL>
+  __device__ __forceinline__ void weigh(q8_f32x4 (&s)[4], float qscale, VAL &&value) {
+    float p[16], mx = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      p[e] = s[e >> 2][e & 3] * qscale;
+      mx = fmaxf(mx, p[e]);
+    }
+    const float m_new = fmaxf(m, kg_max(mx));
+    if (__any(m_new != m)) {
+      const float alpha = __builtin_amdgcn_exp2f(m - m_new);
+      l *= alpha;
+#pragma unroll
+      for (int f = 0; f < VF; ++f) o[f] *= alpha;
+      m = m_new;
+    }
+    // Part 0 is the first 16 bits of a number just below p, part 1 those of a number just below what is left, the last part what is left
+    // then (two parts: rounded): all of them are positive where p is not 0, so that an infinite value comes out with its sign.
+    uint32_t w[8];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      p[e] = __builtin_amdgcn_exp2f(p[e] - m);
+      l += p[e];
+      const uint32_t w0 = __builtin_elementwise_sub_sat(__float_as_uint(p[e]), 1u) & 0xffff0000u;
+      const float r1 = p[e] - __uint_as_float(w0);
+      if constexpr (PARTS == 3) {
+        const uint32_t w1 = __builtin_elementwise_sub_sat(__float_as_uint(r1), 1u) & 0xffff0000u;
+        const float r2 = r1 - __uint_as_float(w1);
+        p[e] = __uint_as_float(part == 0 ? w0 : part == 1 ? w1 : part == 2 ? __float_as_uint(r2) : 0u);
+      } else {
+        p[e] = part == 0 ? __uint_as_float(w0) : r1;
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = q8_pack2(p[2 * e], p[2 * e + 1]);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const q8_bf16x8 pb = __builtin_bit_cast(q8_bf16x8, make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));
+#pragma unroll
+      for (int f = 0; f < VF; ++f) o[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(value(f, i), pb, o[f], 0, 0, 0);
+    }
+  }
+
+  // Pages i0, i0 + step, ... < i1 of a unit.
+  __device__ __forceinline__ void pages(const ag_q8_dev &c, const int32_t *page, int i0, int i1, int step, float qscale) {
+    q8_u32x4 kr[KF], vr[VF];
+    float ks = 1.f, vs = 1.f, ks_next = 1.f, vs_next = 1.f;
+    auto id_of = [&](int i) { return __builtin_amdgcn_readfirstlane(page[i]); };
+    auto there = [&](int p) { return (unsigned)p < (unsigned)c.n_pages; };
+    auto load = [&](const uint8_t *pool, int p, auto &r) {  // every page is read once per step: non-temporal
+      const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)(pool + (size_t)p * (kQ8Block * D)), 0, kQ8Block * D, 0x00020000);
+#pragma unroll
+      for (int f = 0; f < (int)(sizeof(r) / sizeof(r[0])); ++f) r[f] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, lane * 16 + (f & 3) * 1024, f / 4 * 4096, 2);
+    };
+    if (i0 >= i1) return;
+    int id = id_of(i0), next = i0 + step < i1 ? id_of(i0 + step) : 0;
+    bool ok = there(id);
+    if (!ok) id = 0;
+    load(c.k, id, kr);
+    load(c.v, id, vr);
+    ks = c.k_scale[id]; vs = c.v_scale[id];
+    for (int i = i0; i < i1; i += step) {
+      const bool more = i + step < i1, now = ok;
+      id = next;
+      if (more) {
+        ok = there(id);
+        if (!ok) id = 0;
+        next = i + 2 * step < i1 ? id_of(i + 2 * step) : 0;
+        ks_next = c.k_scale[id]; vs_next = c.v_scale[id];
+      }
+      q8_f32x4 s[4];
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        q8_f32x4 x[2] = {q8_f32x4{0.f, 0.f, 0.f, 0.f}, q8_f32x4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+        for (int cc = 0; cc < KC; ++cc)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) score(x, cc, h, q8_widen(kr[a * KC + cc][2 * h], kr[a * KC + cc][2 * h + 1], ks));
+        s[a] = x[0] + x[1];
+      }
+      if (more) load(c.k, id, kr);
+      if (!now) {  // (a page id outside the pool: rows that are not there)
+#pragma unroll
+        for (int a = 0; a < 4; ++a) s[a] = q8_f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      }
+      weigh(s, qscale, [&](int f, int h) { return q8_widen(vr[f][2 * h], vr[f][2 * h + 1], now ? vs : 1.f); });
+      if (more) load(c.v, id, vr);
+      ks = ks_next; vs = vs_next;
+    }
+  }
+
+  // The tail's n rows and the new token as row n (nk: this lane's part of its turned key); `append`: the new row stays.
+  __device__ __forceinline__ void tail(const dec_args &a, int u, int n, int block, bool append, const uint4 (&nk)[KC][2]) {
+    uint16_t *kt = a.c.k_tail + (size_t)u * kQ8Block * D, *vt = a.c.v_tail + (size_t)u * kQ8Block * D;
+    const uint16_t *vn = a.v_new + (size_t)u * D;
+    // rows that are not there are not read (addresses past the descriptor's end give zeros)
+    auto rsrc_of = [](const uint16_t *p) { return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, kQ8Block * D * 2, 0x00020000); };
+    auto load = [](__amdgpu_buffer_rsrc_t rsrc, int at, bool there) {
+      return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, there ? at : 1 << 24, 0, 0));
+    };
+    const __amdgpu_buffer_rsrc_t k_rsrc = rsrc_of(kt), v_rsrc = rsrc_of(vt);
+    uint4 kr[4][KC][2], vr[VF][2];
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+#pragma unroll
+      for (int c = 0; c < KC; ++c)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) kr[x][c][s] = load(k_rsrc, ((x * KC + c) * 64 + lane) * 32 + 16 * s, 16 * x + col < n);
+#pragma unroll
+    for (int f = 0; f < VF; ++f)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) vr[f][i] = load(v_rsrc, (f * 64 + lane) * 32 + 16 * i, 32 * i + 4 * g < n);
+    uint16_t nv[VF];
+#pragma unroll
+    for (int f = 0; f < VF; ++f) nv[f] = vn[16 * f + col];
+    // the new row joins: row n = 16 (n / 16) + col for K, = 16 i + 4 g + n % 4 for V
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      if (16 * x + col == n) {
+#pragma unroll
+        for (int c = 0; c < KC; ++c)
+#pragma unroll
+          for (int s = 0; s < 2; ++s) kr[x][c][s] = nk[c][s];
+      }
+    const bool fills = append && n == kQ8Block - 1;  // the block is full: it goes to its page; else the row joins the tail
+    if (append && !fills && col == (n & 15)) {
+#pragma unroll
+      for (int c = 0; c < KC; ++c)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) *reinterpret_cast<uint4 *>(kt + q8_k_at<D>(n, c, g) * 16 + 8 * h) = nk[c][h];
+    }
+    q8_f32x4 s[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      q8_f32x4 y[2] = {q8_f32x4{0.f, 0.f, 0.f, 0.f}, q8_f32x4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+      for (int c = 0; c < KC; ++c)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) score(y, c, h, __builtin_bit_cast(q8_bf16x8, kr[x][c][h]));
+      s[x] = y[0] + y[1];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int row = 16 * x + 4 * g + r;
+        if (row > n) s[x][r] = -INFINITY;
+        // the new token: alone its weight is 1 whatever its score is; a score that overflowed to -infinity counts as the least number
+        if (row == n) s[x][r] = n == 0 && block == 0 ? 0.f : (s[x][r] == -INFINITY ? kQ8EmptyMax : s[x][r]);
+      }
+    }
+    auto narrow = [](const uint4 &x, const uint4 &y, float inv) {
+      return make_uint4(q8_narrow(x.x, x.y, inv), q8_narrow(x.z, x.w, inv), q8_narrow(y.x, y.y, inv), q8_narrow(y.z, y.w, inv));
+    };
+    auto wave_max = [](uint32_t top) {
+#pragma unroll
+      for (int x = 32; x > 0; x >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, x, 64));
+      return q8_exponent(__builtin_amdgcn_readfirstlane(top));
+    };
+    auto top4 = [](uint32_t top, const uint4 &w) { return q8_top(q8_top(q8_top(q8_top(top, w.x), w.y), w.z), w.w); };
+    const int id = fills ? a.c.page[(size_t)u * a.c.max_blocks + block] : 0;
+    if (fills) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int c = 0; c < KC; ++c) top = top4(top4(top, kr[x][c][0]), kr[x][c][1]);
+      const int e = wave_max(top);
+      const float inv = q8_pow2(-e);
+      uint4 *to = reinterpret_cast<uint4 *>(a.c.k + (size_t)id * kQ8Block * D) + lane;
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int c = 0; c < KC; ++c) to[(x * KC + c) * 64] = narrow(kr[x][c][0], kr[x][c][1], inv);
+      if (lane == 0) a.c.k_scale[id] = q8_pow2(e);
+    }
+    uint32_t old[8], mine[8];  // halves of word y (rows 16 (y / 2) + 4 g + 2 (y % 2) + 0, 1) that are rows before n, and row n
+#pragma unroll
+    for (int y = 0; y < 8; ++y) {
+      const int r = 16 * (y / 2) + 4 * g + 2 * (y & 1);
+      old[y] = (r < n ? 0xffffu : 0u) | (r + 1 < n ? 0xffff0000u : 0u);
+      mine[y] = (r == n ? 0xffffu : 0u) | (r + 1 == n ? 0xffff0000u : 0u);
+    }
+#pragma unroll
+    for (int f = 0; f < VF; ++f) {
+      const uint32_t two = (uint32_t)nv[f] * 0x10001u;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        uint4 &w = vr[f][i];
+        w.x = (w.x & old[4 * i]) | (two & mine[4 * i]);
+        w.y = (w.y & old[4 * i + 1]) | (two & mine[4 * i + 1]);
+        w.z = (w.z & old[4 * i + 2]) | (two & mine[4 * i + 2]);
+        w.w = (w.w & old[4 * i + 3]) | (two & mine[4 * i + 3]);
+      }
+    }
+    if (append && !fills && g == ((n >> 2) & 3)) {
+#pragma unroll
+      for (int f = 0; f < VF; ++f) vt[(f * 64 + lane) * 16 + (n >> 4) * 4 + (n & 3)] = nv[f];
+    }
+    weigh(s, a.qscale, [&](int f, int i) { return __builtin_bit_cast(q8_bf16x8, vr[f][i]); });
+    if (fills) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int f = 0; f < VF; ++f) top = top4(top4(top, vr[f][0]), vr[f][1]);
+      const int e = wave_max(top);
+      const float inv = q8_pow2(-e);
+      uint4 *to = reinterpret_cast<uint4 *>(a.c.v + (size_t)id * kQ8Block * D) + lane;
+#pragma unroll
+      for (int f = 0; f < VF; ++f) to[f * 64] = narrow(vr[f][0], vr[f][1], inv);
+      if (lane == 0) a.c.v_scale[id] = q8_pow2(e);
+    }
+  }
+  // The wave's state: per head [max, sum, -, -, o[0 .. D)].
+  __device__ __forceinline__ void leave(float *st) {
+    l = kg_sum(l);
+#pragma unroll
+    for (int f = 0; f < VF; ++f) {
+      q8_f32x4 x;
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        x[r] = P == 4 ? o[f][r] + column<4>(o[f][r]) + column<8>(o[f][r]) : o[f][r] + column<8>(o[f][r]);
+      if (col < G) *reinterpret_cast<q8_f32x4 *>(st + col * SF + 4 + 16 * f + 4 * g) = x;
+    }
+    if (col < G && g == 0) {
+      st[col * SF] = m;
+      st[col * SF + 1] = l;
+    }
+  }
+};
+
+template <int D, int G>
+__global__ __launch_bounds__(NT, 2) void ag_q8_decode_kernel(dec_args a) {
+  typedef wave_q8<D, G> wave_t;
+  constexpr int SF = wave_t::SF;
+  __shared__ __attribute__((aligned(16))) float s_state[NW][G * SF];
+  __shared__ __attribute__((aligned(16))) float s_angles[NW][D];
+  extern __shared__ int32_t s_len[];  // [U] rows held; top bit: another one fits
+  __shared__ int32_t w_sum[NW][4], s_start[2], s_last, s_order;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int U = a.U, wg = blockIdx.x, grid = gridDim.x;
+  const int most = a.c.max_blocks * kQ8Block + kQ8Block - 1;
+
+  // ---- the work list ----
+  auto items_of = [](int n) { return (n & 0x7fffffff) / kQ8Block + 1; };
+  const int per = (U + NT - 1) / NT, u0 = min(U, tid * per), u1 = min(U, u0 + per);  // this thread's units
+  int my_t = 0, max_t = 0;
+  for (int v = u0; v < u1; ++v) {
+    int n = max(0, min(a.c.len[v], most));
+    const int at = n / kQ8Block;
+    if ((n & (kQ8Block - 1)) != kQ8Block - 1 ||
+        (at < a.c.max_blocks && (unsigned)a.c.page[(size_t)v * a.c.max_blocks + at] < (unsigned)a.c.n_pages))
+      n |= (int)0x80000000;
+    s_len[v] = n;
+    my_t += items_of(n);
+    max_t = max(max_t, items_of(n));
+  }
+  int sum;
+  int pre_t = wave_prefix(my_t, sum);
+  for (int x = 32; x > 0; x >>= 1) max_t = max(max_t, __shfl_xor(max_t, x, 64));
+  if (lane == 0) { w_sum[wave][0] = sum; w_sum[wave][1] = max_t; }
+  __syncthreads();
+  // The lengths may only change once every workgroup has read them: each counts its arrival, the last one writes them at its end.
+  const int groups = grid >= kArriveSplit ? kDecodeArriveGroups : 1;
+  if (tid == 0)
+    s_order = __hip_atomic_fetch_add(a.arrived + (groups == 1 ? 0 : kDecodeArriveStride * (1 + wg % kDecodeArriveGroups)), 1, __ATOMIC_RELAXED,
+                                   __HIP_MEMORY_SCOPE_AGENT);
+  int total = 0;
+  max_t = 0;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    if (w < wave) pre_t += w_sum[w][0];
+    total += w_sum[w][0];
+    max_t = max(max_t, w_sum[w][1]);
+  }
+  // pieces of `piece` items: the fewest rounds of the waves for which every piece has a workgroup (sure for r2 rounds, where U < grid)
+  const int r1 = max(1, (total + NW * grid - 1) / (NW * grid)), r2 = U < grid ? max(r1, (total + NW * (grid - U) - 1) / (NW * (grid - U))) : 0;
+  auto pieces_of = [](int t, int piece) { return (t + piece - 1) / piece; };
+  int my_1 = 0, my_2 = 0;
+  if (U < grid)
+    for (int v = u0; v < u1; ++v) {
+      my_1 += pieces_of(items_of(s_len[v]), r1 * NW);
+      my_2 += pieces_of(items_of(s_len[v]), r2 * NW);
+    }
+  int sum_1, sum_2;
+  int pre_1 = wave_prefix(my_1, sum_1), pre_2 = wave_prefix(my_2, sum_2);
+  if (lane == 0) { w_sum[wave][2] = sum_1; w_sum[wave][3] = sum_2; }
+  __syncthreads();
+  int all_1 = 0, all_2 = 0;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    if (w < wave) { pre_1 += w_sum[w][2]; pre_2 += w_sum[w][3]; }
+    all_1 += w_sum[w][2];
+    all_2 += w_sum[w][3];
+  }
+  const bool by_1 = U < grid && all_1 <= grid;
+  const int rounds = by_1 ? r1 : r2, piece = rounds * NW;
+  // ... unless so many units are cut that the remainders of their last pieces weigh more than equal ranges cost
+  const bool by_piece = U < grid && (rounds <= 2 || 4 * U <= grid);
+  int team = NW;
+  while (team > 1 && U * team > grid * NW) team /= 2;
+  const bool by_team = !by_piece && U * team <= grid * NW && max_t <= kTeamRounds * team;
+  const int quota = (total + grid - 1) / grid;
+  int u = 0, sub = 0;
+  bool idle;
+  const int x = by_piece ? wg : wg * quota;
+  if (by_team) {
+    u = wg * (NW / team) + wave / team;
+    idle = wg * (NW / team) >= U;
+  } else {
+    team = NW;
+    idle = x >= (by_piece ? (by_1 ? all_1 : all_2) : total);
+    int at = by_piece ? (by_1 ? pre_1 : pre_2) : pre_t;
+    const int mine = by_piece ? (by_1 ? my_1 : my_2) : my_t;
+    if (at <= x && x < at + mine) {  // exactly one thread, if there is one
+      int v = u0;
+      for (;; ++v) {
+        const int t = by_piece ? pieces_of(items_of(s_len[v]), piece) : items_of(s_len[v]);
+        if (x < at + t) break;
+        at += t;
+      }
+      s_start[0] = v;
+      s_start[1] = x - at;
+    }
+    __syncthreads();
+    if (!idle) { u = s_start[0]; sub = s_start[1]; }
+  }
+
+  const int wt = team == NW ? wave : wave & (team - 1);
+  int left = idle || by_piece || by_team ? 0 : min(quota, total - x), at = x;
+  auto segment = [&]() {
+    u = __builtin_amdgcn_readfirstlane(u);
+    const bool mine = u < U;
+    const int sl = mine ? __builtin_amdgcn_readfirstlane(s_len[u]) : 0;
+    const int n = sl & 0x7fffffff, nb = n / kQ8Block, T = nb + 1;
+    int t0 = 0, t1 = mine ? T : 0, n_rec = 1, my_rec = 0, rec0 = 0;
+    if (by_piece) {
+      n_rec = pieces_of(T, piece);
+      my_rec = sub;
+      rec0 = wg - sub;
+      t0 = sub * piece;
+      t1 = min(T, t0 + piece);
+    } else if (!by_team) {
+      t0 = sub;
+      t1 = min(T, t0 + left);
+      left -= t1 - t0;
+      const int first = at - t0;
+      at += t1 - t0;
+      if (t0 > 0 || t1 < T) {
+        const int g0 = first / quota, g1 = (first + T - 1) / quota;
+        n_rec = g1 - g0 + 1;
+        my_rec = wg - g0;
+        rec0 = g0;
+      }
+    }
+    wave_t wv;
+    int own_lane = lane;  // (unknown to the compiler, which would compute all addresses ahead of the loop and keep them in memory)
+    asm volatile("" : "+v"(own_lane));
+    wv.init(own_lane);
+    const int i0 = t0 + wt, ip = min(t1, nb);
+    const bool has_tail = mine && t1 == T && (nb - t0) % team == wt;
+    if (i0 < ip || has_tail) {
+      const int32_t *page = a.c.page + (size_t)u * a.c.max_blocks;
+      float *angles = nullptr;
+      if (a.rope.table) {  // into LDS: the query and the new key turn by the same
+        const q8_rows rows = q8_rope_rows(a.rope, u / a.Hkv, a.err);
+        angles = s_angles[wave];
+        if (own_lane < D / 2) {
+          const float *row = q8_angle_row(a.rope, rows, own_lane, D) + own_lane;
+          angles[own_lane] = row[0];
+          angles[D / 2 + own_lane] = row[D / 2];
+        }
+        __builtin_amdgcn_wave_barrier();
+      }
+      wv.query(a.q + (size_t)u * G * D, angles);
+      uint4 nk[wave_t::KC][2];
+      if (has_tail) {
+        q8_eight y[wave_t::KC][2];
+        wv.vector(y, a.k_new + (size_t)u * D, angles);
+#pragma unroll
+        for (int c = 0; c < wave_t::KC; ++c)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) nk[c][h] = y[c][h].bf16();
+      }
+      wv.pages(a.c, page, i0, ip, team, a.qscale);
+      if (has_tail) {
+        const bool flag = !a.new_flags || a.new_flags[u] != 0;
+        if (flag && sl >= 0 && lane == 0) atomicOr(a.err, 1);
+        wv.tail(a, u, n & (kQ8Block - 1), nb, flag && sl < 0, nk);
+      }
+    }
+    wv.leave(s_state[wave]);
+    __syncthreads();
+    // ---- merge the team's waves; thread -> (head, two neighbouring columns) ----
+    int e0 = lane;
+    asm volatile("" : "+v"(e0));  // (as above)
+    e0 += wt * 64;
+    auto store_out = [&](int gg, int d, float A0, float A1, float L) {
+      const float inv = 1.f / L;
+      *reinterpret_cast<uint32_t *>(a.out + ((size_t)u * G + gg) * D + d) = q8_pack2(A0 * inv, A1 * inv);
+    };
+    auto rec_at = [&](int k) {
+      const int id = by_piece ? rec0 + k : 2 * (rec0 + k) + (k == 0 ? 1 : 0);
+      return a.rec + (size_t)id * G * (D + 2);
+    };
+    if (mine)
+      for (int e = e0; e < G * D / 2; e += team * 64) {
+        const int gg = e / (D / 2), d = 2 * (e - gg * (D / 2));
+        float M = kQ8EmptyMax, L = 0.f, A0 = 0.f, A1 = 0.f;
+        const int w0 = wave - wt;
+        for (int w = 0; w < team; ++w) M = fmaxf(M, s_state[w0 + w][gg * SF]);
+        for (int w = 0; w < team; ++w) {
+          const float *st = s_state[w0 + w] + gg * SF;
+          if (st[1] == 0.f) continue;  // (a wave without rows)
+          const float f = __builtin_amdgcn_exp2f(st[0] - M);
+          L = fmaf(f, st[1], L);
+          A0 = fmaf(f, st[4 + d], A0);
+          A1 = fmaf(f, st[5 + d], A1);
+        }
+        if (n_rec == 1) {
+          store_out(gg, d, A0, A1, L);
+        } else {
+          float *r = rec_at(my_rec) + gg * (D + 2);
+          put_pair(r + d, A0, A1);
+          if (d == 0) put_pair(r + D, M, L);
+        }
+      }
+    if (!by_team && n_rec > 1) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's part of the record is in memory
+      __syncthreads();
+      if (tid == 0) s_last = __hip_atomic_fetch_add(&a.tickets[u], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == n_rec - 1;
+      __syncthreads();
+      if (s_last) {  // all pieces are there: they are added in order
+        if (tid == 0) a.tickets[u] = 0;
+        for (int e = e0; e < G * D / 2; e += NT) {
+          const int gg = e / (D / 2), d = 2 * (e - gg * (D / 2));
+          float M = kQ8EmptyMax, L = 0.f, A0 = 0.f, A1 = 0.f;
+          for (int k0 = 0; k0 < n_rec; k0 += 8) {
+            float2 ml[8], o[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const float *r = rec_at(min(k0 + j, n_rec - 1)) + gg * (D + 2);
+              ml[j] = get_pair(r + D);
+              o[j] = get_pair(r + d);
+            }
+            float M_new = M;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) M_new = fmaxf(M_new, ml[j].x);
+            const float keep = __builtin_amdgcn_exp2f(M - M_new);
+            M = M_new;
+            L *= keep; A0 *= keep; A1 *= keep;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              if (k0 + j >= n_rec) break;
+              const float w = __builtin_amdgcn_exp2f(ml[j].x - M);
+              L = fmaf(w, ml[j].y, L);
+              A0 = fmaf(w, o[j].x, A0);
+              A1 = fmaf(w, o[j].y, A1);
+            }
+          }
+          store_out(gg, d, A0, A1, L);
+        }
+      }
+    }
+    ++u;
+    sub = 0;
+  };
+  if (!idle)
+    for (;;) {  // (one segment, but where a range covers several units)
+      segment();
+      if (left <= 0) break;
+      __syncthreads();  // the states have been read
+    }
+  // ---- the last workgroup to arrive counts the appended rows ----
+  __syncthreads();
+  if (tid == 0) {
+    int last = grid - 1, order = s_order;
+    if (groups > 1) {
+      const int mine = (grid - wg % kDecodeArriveGroups + kDecodeArriveGroups - 1) / kDecodeArriveGroups;
+      order = order == mine - 1 ? __hip_atomic_fetch_add(a.arrived, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : -1;
+      last = kDecodeArriveGroups - 1;
+    }
+    s_last = order == last;
+  }
+  __syncthreads();
+  if (!s_last) return;
+  for (int v = tid; v < U; v += NT)
+    if (s_len[v] < 0 && (!a.new_flags || a.new_flags[v] != 0)) a.c.len[v] = (s_len[v] & 0x7fffffff) + 1;
+  if (tid <= kDecodeArriveGroups) a.arrived[kDecodeArriveStride * tid] = 0;
+}
+
+template <int D, int G>
+hipError_t launch(ag_ctx *ctx, hipStream_t s, const dec_args &a) {
+  // one workgroup per CU, and no more than the step can have pieces
+  const int64_t most = a.U + (int64_t)a.U * (a.c.max_blocks + 1) / NW;
+  const int grid = (int)std::min<int64_t>(ctx->num_cu, most);
+  static std::atomic<bool> allowed[64];
+  const hipError_t e = ag_q8_allow_lds(ctx->device, allowed, &ag_q8_decode_kernel<D, G>, (size_t)kDecodeMaxUnits * 4);
+  if (e != hipSuccess) return e;
+  AG_LAUNCH(ag_time_kernel(ctx, AG_K_Q8_DECODE), (ag_q8_decode_kernel<D, G>), dim3(grid), dim3(NT), (size_t)a.U * 4, s, a);
+  return hipGetLastError();
+}
+template <int D>
+hipError_t launch_g(int G, ag_ctx *ctx, hipStream_t s, const dec_args &a) {
+  switch (G) {
+    case 1: return launch<D, 1>(ctx, s, a);
+    case 2: return launch<D, 2>(ctx, s, a);
+    case 4: return launch<D, 4>(ctx, s, a);
+    case 8: return launch<D, 8>(ctx, s, a);
+  }
+  return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+size_t ag_ws_q8_decode_floats(int num_cu, int G, int D) { return (size_t)2 * num_cu * G * (D + 2); }
+
+hipError_t ag_launch_q8_decode(ag_ctx *ctx, hipStream_t s, const void *q, const void *k_new, const void *v_new, const uint8_t *new_flags,
+                               int B, int Hq, int Hkv, int D, const ag_rope_dev &rope, float scale, const ag_q8_dev &cache, void *out, float *rec) {
+  dec_args a;
+  a.q = (const uint16_t *)q; a.k_new = (const uint16_t *)k_new; a.v_new = (const uint16_t *)v_new; a.new_flags = new_flags; a.out = (uint16_t *)out;
+  a.c = cache; a.rope = rope; a.rec = rec;
+  a.tickets = ctx->decode_tickets; a.arrived = ctx->decode_tickets + kDecodeMaxUnits; a.err = ctx->d_err;
+  a.U = B * Hkv; a.Hkv = Hkv; a.qscale = scale * kLog2e;
+  return D == 128 ? launch_g<128>(Hq / Hkv, ctx, s, a) : launch_g<64>(Hq / Hkv, ctx, s, a);
+}

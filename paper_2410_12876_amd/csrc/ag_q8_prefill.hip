@@ -1,0 +1,434 @@
+// Attention of many new tokens over the paged 8-bit cache as it stood before the call, and over themselves.
+//
+// For new token j of a unit the visible rows are: all rows that the cache held, the call's own kept tokens before j, and j itself.
+// ag_q8_fill_kernel (launched first) leaves the tail's rows and the kept tokens, turned and packed, as tiles of 64 rows in f16;
+// the full blocks of the cache are read as they are.  So the keys of a unit are one sequence of tiles -- its pages, then those --
+// of which row j sees the first `bound_j` rows; an evicted token's own key and value, which are in none of them, are what its state starts from.
+//   * A workgroup of 4 waves owns 128 query rows of a unit (token by token, the group's heads of a token side by side) and every wave 32 of
+//     them, with a lane owning one column: S^T = K q^T, O^T = V^T p^T on v_mfma_f32_32x32x16_bf16, P passes from the first product's
+//     accumulators into the second one's operand without leaving the lane.
+//   * A tile's 64 rows go through registers into LDS in the order of the fragments; 8-bit codes become f16 there (exactly,
+//     one instruction for two values), once for the 128 rows.  The next tile's loads are in flight meanwhile.
+//   * Both products are in f16, whose 11 bits keep scores and weights to 2^-12 of themselves (in bf16, 2^-9: an output row's error grew from 1.7e-3
+//     to 2.9e-3 of its size, and with scores of 7 times the usual spread a weight was off by a hundredth).  Its narrow range is why queries and
+//     tiles carry exponents; tiles of too different values are taken row by row on the vector ALU.
+//   * No maximum is taken in the common case: weights are formed against the reference as it stands, and only if their sum passes 2^15 is
+//     it moved.
+//   * Few items and long caches: the tiles of an item are cut into up to n_split pieces, whose states a second kernel adds up.
+#include <algorithm>
+
+#include "ag_q8.h"
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kRows = 128;     // query rows of a workgroup
+constexpr int kMinTiles = 4;   // tiles of a piece, at least
+constexpr int kMaxSplit = 32;
+
+struct pf_args {
+  const uint16_t *q, *k, *v;
+  uint16_t *out;
+  const uint64_t *words;
+  const int32_t *blk_off;
+  const uint16_t *tiles;
+  const uint32_t *info;
+  const ag_q8_meta *meta;
+  ag_q8_dev c;
+  ag_rope_dev rope;
+  float *part;    // [item][piece][kRows][D + 2]
+  int32_t *err;
+  int U, Hq, Hkv, L, nw, n_blk, n_qt, n_split;
+  float qscale;
+};
+
+// Kept tokens of the call before token j, and whether j is appended itself.
+__device__ __forceinline__ int rank_of(const pf_args &a, int u, int j, int added, bool &kept) {
+  int r = j;
+  kept = true;
+  if (a.blk_off) {
+    const uint64_t w = a.words[(size_t)u * a.nw + (j >> 6)];
+    r = a.blk_off[(size_t)u * (a.nw + 1) + (j >> 6)] + __popcll(w & ((1ull << (j & 63)) - 1));
+    kept = (w >> (j & 63)) & 1;
+  }
+  kept = kept && r < added;
+  return min(r, added);
+}
+struct pf_cut {
+  int tiles, per, pieces;  // tiles of an item, of a piece; pieces
+};
+__device__ __forceinline__ pf_cut cut_of(const pf_args &a, const ag_q8_meta &m, int u, int qt, int G) {
+  const int last = min(a.L - 1, (qt * kRows + kRows - 1) / G);
+  bool kept;
+  const int rows = m.held + rank_of(a, u, last, m.added, kept);  // (+ 1 if kept: below)
+  pf_cut c;
+  c.tiles = m.blocks + (rows + (kept ? 1 : 0) + kQ8Block - 1) / kQ8Block;
+  c.per = max(kMinTiles, (c.tiles + a.n_split - 1) / a.n_split);
+  c.pieces = max(1, (c.tiles + c.per - 1) / c.per);
+  return c;
+}
+
+__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32, 64); }
+
+template <int D, int G>
+__global__ __launch_bounds__(256, 2) void ag_q8_prefill_kernel(pf_args a) {
+  constexpr int KC = D / 64, KS = D / 16, DT = D / 32, HALF = kQ8Block * D;  // values of K (V) in a tile
+  constexpr int NP = KS;  // 16-byte pieces of a bf16 tile per thread
+  extern __shared__ __attribute__((aligned(1024))) uint16_t smem[];  // two tiles: K fragments, V fragments
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 31, h = lane >> 5;
+  // block -> (piece, query tile, unit): long query tiles first, units next to each other
+  int id = blockIdx.x;
+  const int u = id % a.U;
+  id /= a.U;
+  const int piece = id % a.n_split, qt = a.n_qt - 1 - id / a.n_split;
+  const ag_q8_meta meta = a.meta[u];
+  const pf_cut cut = cut_of(a, meta, u, qt, G);
+  const int t0 = piece * cut.per, t1 = min(cut.tiles, t0 + cut.per);
+  if (piece > 0 && t0 >= t1) return;
+
+  // ---- this lane's query row ----
+  const int rows = a.L * G, b = u / a.Hkv;
+  auto row_of = [&](int c) { return qt * kRows + wave * 32 + c; };
+  auto token_of = [&](int row) { return min(row / G, a.L - 1); };
+  auto q_of = [&](int row) { return (((size_t)b * a.Hq + (size_t)(u % a.Hkv) * G + row % G) * a.L + token_of(row)) * D; };
+  const int j = token_of(row_of(col));
+  const size_t k_at = ((size_t)u * a.L + j) * D;
+  bool kept;
+  const int rank = rank_of(a, u, j, meta.added, kept);
+  const int bound = meta.held + rank + (kept ? 1 : 0);  // visible rows of those tiles
+  // The query in f16 times 2^eq (11 bits; bf16 would lose up to 2^-9 of a turned value, and the scores as much of themselves)
+  q8_rows at = {0, 0, 0};
+  auto angles = [&](int i) { return q8_angles4(a.rope, at, i, D); };
+  if (a.rope.table) at = q8_rope_rows(a.rope, (int64_t)b * a.L + j, a.err);
+  auto vector = [&](q8_eight (&y)[KS], const uint16_t *x) {  // this lane's half of a row, turned
+    uint4 raw[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) raw[ks] = *reinterpret_cast<const uint4 *>(x + 16 * ks + 8 * h);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+      y[ks] = a.rope.table ? q8_turn8<D>(angles, 16 * ks + 8 * h, raw[ks], raw[ks ^ (KS / 2)]) : q8_floats(raw[ks]);
+  };
+  q8_f16x8 qx[KS];
+  int eq;
+  {
+    q8_eight y[KS];
+    vector(y, a.q + q_of(row_of(col)));
+    float top = 0.f;  // (infinities are none of a binade's; NaN is passed over)
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) top = fmaxf(top, y[ks].top());
+    top = fmaxf(top, other_half(top));
+    eq = max(kQ8TileMinExp, min(254, max(1, (int)(__float_as_uint(top) >> 23))) - 127 - kQ8TileTop);
+    const float inv = q8_pow2(-eq);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qx[ks] = y[ks].f16(inv);
+  }
+  float m = kQ8EmptyMax, l = 0.f;
+  const bool alone = piece == 0 && !kept;  // an evicted token sees itself
+  if (alone) {
+    q8_eight y[KS];
+    vector(y, a.k + k_at);
+    float s = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s = fmaf((float)qx[ks][i], y[ks].a[i], fmaf((float)qx[ks][4 + i], y[ks].b[i], s));
+    s = (s + other_half(s)) * ldexpf(a.qscale, eq);
+    // seeing nothing else its weight is 1 whatever its score is; a score that overflowed to -infinity counts as the least number
+    m = meta.blocks == 0 && bound == 0 ? 0.f : (s < kQ8EmptyMax ? kQ8EmptyMax : s);
+    l = h == 0 ? 1.f : 0.f;  // (summed over the halves at the end)
+  }
+  q8_f32x16 o[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      uint2 w = make_uint2(0, 0);
+      if (alone) w = *reinterpret_cast<const uint2 *>(a.v + k_at + 32 * dt + 8 * x + 4 * h);
+      o[dt][4 * x] = q8_lo(w.x); o[dt][4 * x + 1] = q8_hi(w.x);
+      o[dt][4 * x + 2] = q8_lo(w.y); o[dt][4 * x + 3] = q8_hi(w.y);
+    }
+  // rows that every row of the wave sees, and that one of them sees
+  int see_all = bound, see_one = bound;
+#pragma unroll
+  for (int x = 16; x > 0; x >>= 1) {
+    see_all = min(see_all, __shfl_xor(see_all, x, 64));
+    see_one = max(see_one, __shfl_xor(see_one, x, 64));
+  }
+  see_all = __builtin_amdgcn_readfirstlane(see_all);
+  see_one = __builtin_amdgcn_readfirstlane(see_one);
+
+  const int32_t *page = a.c.page + (size_t)u * a.c.max_blocks;
+  const uint16_t *tiles = a.tiles + (size_t)u * a.n_blk * 2 * HALF;
+  uint4 st[2 * NP];
+  bool have = false;  // the tile asked for is there (a page number outside the pool counts as evicted rows)
+  q8_tile_info info = {0, 0, false};
+  float v_scale = 1.f;
+  // a thread's two pieces of a page's V: rows 16 i + 4 g + 0..3 and 16 i + 4 (g + 2) + 0..3, i < 4, of column 16 f + r
+  const int vf = (tid >> 5) & (D / 16 - 1), vg = (tid >> 4) & 1, v_piece = (vf * 4 + vg) * 16 + (tid & 15);
+  auto rsrc_of = [](const void *p, int bytes) { return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, bytes, 0x00020000); };
+  auto load = [](__amdgpu_buffer_rsrc_t r, int at, int more) { return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(r, at, more, 0)); };
+  auto request = [&](int t) {
+    if (t < meta.blocks) {
+      const int p = page[t];
+      have = (unsigned)p < (unsigned)a.c.n_pages;
+      const int ps = have ? p : 0;
+      auto exponent = [](float x) { return (int)(__builtin_amdgcn_readfirstlane(__float_as_uint(x)) >> 23) - 127; };
+      const int e = exponent(a.c.v_scale[ps]);
+      info = q8_tile_info{exponent(a.c.k_scale[ps]), max(kQ8TileMinExp, e), false};
+      v_scale = q8_pow2(e - info.ev);
+      const __amdgpu_buffer_rsrc_t pk = rsrc_of(a.c.k + (size_t)ps * HALF, HALF), pv = rsrc_of(a.c.v + (size_t)ps * HALF, HALF);
+#pragma unroll
+      for (int x = 0; x < KC; ++x) st[x] = load(pk, tid * 16, x * 4096);
+      st[KC] = load(pv, v_piece * 16, 0);
+      st[KC + 1] = load(pv, v_piece * 16, 512);
+    } else {
+      have = true;
+      info = q8_tile_of(__builtin_amdgcn_readfirstlane(a.info[(size_t)u * a.n_blk + t - meta.blocks]));
+      const __amdgpu_buffer_rsrc_t w = rsrc_of(tiles + (size_t)(t - meta.blocks) * 2 * HALF, 4 * HALF);
+#pragma unroll
+      for (int x = 0; x < NP; ++x) st[x] = load(w, tid * 16, x * 4096);
+    }
+  };
+  auto stage = [&](int t, int buf) {
+    uint16_t *ks = smem + buf * 2 * HALF, *vs = ks + HALF;
+    if (t < meta.blocks) {
+#pragma unroll
+      for (int x = 0; x < KC; ++x) {
+        const int n = tid + 256 * x, r = n & 15, g = (n >> 4) & 3, c = (n >> 6) % KC, ra = (n >> 6) / KC, tt = 16 * ra + r;
+        uint16_t *to = ks + (((tt >> 5) * KS + 4 * c + g) * 64 + (tt & 31)) * 8;
+        *reinterpret_cast<q8_f16x8 *>(to) = q8_widen16(st[x].x, st[x].y, 1.f);
+        *reinterpret_cast<q8_f16x8 *>(to + 32 * 8) = q8_widen16(st[x].z, st[x].w, 1.f);
+      }
+      if (D == 128 || tid < 128) {
+        const uint32_t lo[4] = {st[KC].x, st[KC].y, st[KC].z, st[KC].w}, hi[4] = {st[KC + 1].x, st[KC + 1].y, st[KC + 1].z, st[KC + 1].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<q8_f16x8 *>(vs + (((vf >> 1) * 4 + i) * 64 + vg * 32 + (vf & 1) * 16 + (tid & 15)) * 8) = q8_widen16(lo[i], hi[i], v_scale);
+      }
+    } else {
+#pragma unroll
+      for (int x = 0; x < NP; ++x) reinterpret_cast<uint4 *>(ks)[tid + 256 * x] = st[x];
+    }
+  };
+
+  bool any_odd = false;
+  if (t0 < t1) {
+    request(t0);
+    stage(t0, 0);
+  }
+  for (int t = t0; t < t1; ++t) {
+    const int buf = (t - t0) & 1;
+    const bool now = have;
+    const q8_tile_info it = info;
+    __syncthreads();
+    if (t + 1 < t1) request(t + 1);
+    const int first = (t - meta.blocks) * kQ8Block;  // the tile's first row among the bf16 rows
+    any_odd |= it.odd;
+    if (now && first < see_one && !it.odd) {
+      const uint16_t *ks = smem + buf * 2 * HALF, *vs = ks + HALF;
+      q8_f32x16 s[2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[x][i] = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < KS; ++kk)
+          s[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const q8_f16x8 *>(ks + ((x * KS + kk) * 64 + lane) * 8), qx[kk], s[x], 0, 0, 0);
+      }
+      // s[x][i]: row 32 x + 8 (i / 4) + 4 h + i % 4 of the tile.  The state is kept relative to m, the largest score plus its tile's ev: a
+      // tile's weights are 2^(score + ev - m), at most 2^15, its values v 2^-ev, and its part of the row sum is 2^-ev the sum of its weights.
+      const float f = fmaxf(ldexpf(a.qscale, eq + it.ek), 1.17549435e-38f), ev = (float)it.ev;
+      if (t >= meta.blocks && first + kQ8Block > see_all) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (first + 32 * x + 8 * (i / 4) + 4 * h + i % 4 >= bound) s[x][i] = -INFINITY;
+      }
+      q8_f16x2 p[2][8];
+      float sum;
+      auto weigh = [&] {
+        const float off = ev - m;
+        sum = 0.f;
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int i = 0; i < 16; i += 2) {
+            const q8_f32x2 w = {__builtin_amdgcn_exp2f(fmaf(s[x][i], f, off)), __builtin_amdgcn_exp2f(fmaf(s[x][i + 1], f, off))};
+            sum += w[0] + w[1];
+            p[x][i / 2] = __builtin_convertvector(w, q8_f16x2);
+            if (i % 8 == 6) __builtin_amdgcn_sched_barrier(0);  // (all 32 at once would not fit the registers)
+          }
+      };
+      weigh();
+      if (__any(!(sum <= 32768.f))) {  // the reference is too far below (or nothing yet): a new one, and the weights again
+        float mx = -INFINITY;
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[x][i]);
+        mx = fmaf(fmaxf(mx, other_half(mx)), f, ev);
+        const float both = fmaxf(sum <= 32768.f ? 0.f : 1.f, other_half(sum <= 32768.f ? 0.f : 1.f));
+        const float m_new = both > 0.f ? fmaxf(m, mx) : m;  // (a row's own reference alone: no row depends on its neighbours)
+        const float alpha = __builtin_amdgcn_exp2f(m - m_new);
+        l *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[dt] *= alpha;
+        m = m_new;
+        weigh();
+      }
+      l += ldexpf(sum, -it.ev);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const q8_f16x2 *w = &p[i >> 1][4 * (i & 1)];
+          const q8_f16x8 pb = {w[0][0], w[0][1], w[1][0], w[1][1], w[2][0], w[2][1], w[3][0], w[3][1]};
+          o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const q8_f16x8 *>(vs + ((dt * 4 + i) * 64 + lane) * 8), pb, o[dt], 0, 0, 0);
+        }
+    }
+    if (t + 1 < t1) stage(t + 1, buf ^ 1);
+  }
+  if (any_odd) {  // rare: tiles with values that are not finite, or of too different sizes; row by row in 32 bits
+    const float f = ldexpf(a.qscale, eq);
+    for (int t = max(t0, meta.blocks); t < t1; ++t) {
+      const int first = (t - meta.blocks) * kQ8Block;
+      if (!q8_tile_of(a.info[(size_t)u * a.n_blk + t - meta.blocks]).odd) continue;
+      const uint16_t *tk = tiles + (size_t)(t - meta.blocks) * 2 * HALF, *tv = tk + HALF;
+      for (int r = 0; r < kQ8Block && first + r < see_one; ++r) {
+        float s = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < KS; ++kk) {
+          const q8_eight y = q8_floats(*reinterpret_cast<const uint4 *>(tk + (((r >> 5) * KS + kk) * 64 + h * 32 + (r & 31)) * 8));
+          q8_f16x8 q = qx[kk];
+          asm volatile("" : "+v"(q));  // (or the compiler would keep all of the query in 32 bits across the loop)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s = fmaf((float)q[i], y.a[i], fmaf((float)q[4 + i], y.b[i], s));
+        }
+        s = (s + other_half(s)) * f;
+        if (first + r < bound) {
+          const float m_new = fmaxf(m, s < kQ8EmptyMax ? kQ8EmptyMax : s);
+          const float alpha = __builtin_amdgcn_exp2f(m - m_new), w = __builtin_amdgcn_exp2f(s - m_new);
+          m = m_new;
+          l = fmaf(l, alpha, h == 0 ? w : 0.f);
+          // row r: step r / 16, half (r / 4) % 2, element 4 ((r / 8) % 2) + r % 4 of a column's piece
+          const uint16_t *vr = tv + ((r >> 4) * 64 + ((r >> 2) & 1) * 32) * 8 + ((r >> 3) & 1) * 4 + (r & 3);
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              o[dt][i] = fmaf(o[dt][i], alpha, w * __uint_as_float((uint32_t)vr[(dt * 4 * 64 + 8 * (i / 4) + 4 * h + i % 4) * 8] << 16));
+        }
+      }
+    }
+  }
+  l += other_half(l);
+  int end_lane = lane;
+  asm volatile("" : "+v"(end_lane));  // (or the addresses below would be kept in registers all the way)
+  const int end_row = row_of(end_lane & 31), end_h = end_lane >> 5;
+  if (cut.pieces == 1) {
+    if (end_row < rows) {
+      const float inv = 1.f / l;
+      uint16_t *to = a.out + q_of(end_row) + 4 * end_h;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          *reinterpret_cast<uint2 *>(to + 32 * dt + 8 * x) =
+              make_uint2(q8_pack2(o[dt][4 * x] * inv, o[dt][4 * x + 1] * inv), q8_pack2(o[dt][4 * x + 2] * inv, o[dt][4 * x + 3] * inv));
+    }
+    return;
+  }
+  float *to = a.part + ((((size_t)qt * a.U + u) * a.n_split + piece) * kRows + wave * 32 + (end_lane & 31)) * (D + 4);
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      *reinterpret_cast<float4 *>(to + 32 * dt + 8 * x + 4 * end_h) = make_float4(o[dt][4 * x], o[dt][4 * x + 1], o[dt][4 * x + 2], o[dt][4 * x + 3]);
+  if (end_h == 0) *reinterpret_cast<float2 *>(to + D) = make_float2(m, l);
+}
+
+// Adds up the pieces of the items that were cut: thread = four columns of a query row.
+template <int D, int G>
+__global__ __launch_bounds__(256) void ag_q8_prefill_merge_kernel(pf_args a) {
+  constexpr int TPR = D / 4;
+  const int per = 256 / TPR, n_wg = kRows / per;
+  int id = blockIdx.x;
+  const int part = id % n_wg;
+  id /= n_wg;
+  const int u = id % a.U, qt = id / a.U;
+  const ag_q8_meta meta = a.meta[u];
+  const pf_cut cut = cut_of(a, meta, u, qt, G);
+  if (cut.pieces == 1) return;
+  const int r = part * per + threadIdx.x / TPR, d = (threadIdx.x % TPR) * 4, row = qt * kRows + r;
+  if (row >= a.L * G) return;
+  const float *from = a.part + (((size_t)qt * a.U + u) * a.n_split * kRows + r) * (D + 4);
+  float M = kQ8EmptyMax, L = 0.f;
+  for (int p = 0; p < cut.pieces; ++p) M = fmaxf(M, from[(size_t)p * kRows * (D + 4) + D]);
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int p = 0; p < cut.pieces; ++p) {
+    const float *f = from + (size_t)p * kRows * (D + 4);
+    const float4 x = *reinterpret_cast<const float4 *>(f + d);
+    const float2 ml = *reinterpret_cast<const float2 *>(f + D);
+    const float w = __builtin_amdgcn_exp2f(ml.x - M);
+    L = fmaf(w, ml.y, L);
+    o.x = fmaf(w, x.x, o.x); o.y = fmaf(w, x.y, o.y); o.z = fmaf(w, x.z, o.z); o.w = fmaf(w, x.w, o.w);
+  }
+  const float inv = 1.f / L;
+  const int j = row / G, b = u / a.Hkv;
+  *reinterpret_cast<uint2 *>(a.out + (((size_t)b * a.Hq + (size_t)(u % a.Hkv) * G + row % G) * a.L + j) * D + d) =
+      make_uint2(q8_pack2(o.x * inv, o.y * inv), q8_pack2(o.z * inv, o.w * inv));
+}
+
+// Pieces an item may be cut into: so many that the launch fills the workgroups the chip holds at once, from what the cache can hold at most.
+int splits(int num_cu, int U, int n_qt, int max_tiles) {
+  const int64_t items = (int64_t)U * n_qt;
+  const int64_t want = (2 * num_cu + items - 1) / items;
+  return (int)std::max<int64_t>(1, std::min<int64_t>({want, (int64_t)kMaxSplit, (int64_t)(max_tiles + kMinTiles - 1) / kMinTiles}));
+}
+
+template <int D, int G>
+hipError_t launch(ag_ctx *ctx, hipStream_t s, const pf_args &a) {
+  const dim3 grid((unsigned)(a.U * a.n_qt * a.n_split));
+  static std::atomic<bool> allowed[64];
+  const hipError_t e = ag_q8_allow_lds(ctx->device, allowed, &ag_q8_prefill_kernel<D, G>, 4 * kQ8Block * D * 2);
+  if (e != hipSuccess) return e;
+  AG_LAUNCH(ag_time_kernel(ctx, AG_K_Q8_PREFILL), (ag_q8_prefill_kernel<D, G>), grid, dim3(256), 4 * kQ8Block * D * 2, s, a);
+  if (a.n_split > 1)
+    hipLaunchKernelGGL((ag_q8_prefill_merge_kernel<D, G>), dim3((unsigned)(a.U * a.n_qt * (kRows / (256 / (D / 4))))), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+template <int D>
+hipError_t launch_g(int G, ag_ctx *ctx, hipStream_t s, const pf_args &a) {
+  switch (G) {
+    case 1: return launch<D, 1>(ctx, s, a);
+    case 2: return launch<D, 2>(ctx, s, a);
+    case 4: return launch<D, 4>(ctx, s, a);
+    case 8: return launch<D, 8>(ctx, s, a);
+  }
+  return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+void ag_q8_prefill_plan(int num_cu, int U, int Hq, int Hkv, int L, int D, int max_blocks, ws_cursor &ws, ag_q8_prefill_ws *w) {
+  w->tiles = ws.take<uint16_t>((size_t)U * ag_q8_fill_blocks(L) * 2 * kQ8Block * D);
+  w->info = ws.take<uint32_t>((size_t)U * ag_q8_fill_blocks(L));
+  w->meta = ws.take<ag_q8_meta>(U);
+  w->n_qt = (int)(((int64_t)L * (Hq / Hkv) + kRows - 1) / kRows);
+  w->n_split = splits(num_cu, U, w->n_qt, max_blocks + ag_q8_fill_blocks(L));
+  w->part = w->n_split > 1 ? ws.take<float>((size_t)U * w->n_qt * w->n_split * kRows * (D + 4)) : nullptr;
+}
+
+hipError_t ag_launch_q8_prefill(ag_ctx *ctx, hipStream_t s, const void *q, const void *k, const void *v, int B, int Hq, int Hkv, int L,
+                                int D, const uint64_t *words, const int32_t *blk_off, const ag_rope_dev &rope, float scale,
+                                const ag_q8_dev &cache, const ag_q8_prefill_ws &w, void *out) {
+  pf_args a;
+  a.q = (const uint16_t *)q; a.k = (const uint16_t *)k; a.v = (const uint16_t *)v; a.out = (uint16_t *)out;
+  a.words = words; a.blk_off = blk_off; a.tiles = w.tiles; a.info = w.info; a.meta = w.meta; a.c = cache; a.rope = rope;
+  a.part = w.part; a.err = ctx->d_err;
+  a.U = B * Hkv; a.Hq = Hq; a.Hkv = Hkv; a.L = L; a.nw = ag_nwords(L); a.n_blk = ag_q8_fill_blocks(L); a.n_qt = w.n_qt; a.n_split = w.n_split;
+  a.qscale = scale * kLog2e;
+  return D == 128 ? launch_g<128>(Hq / Hkv, ctx, s, a) : launch_g<64>(Hq / Hkv, ctx, s, a);
+}
