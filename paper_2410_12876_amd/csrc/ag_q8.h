@@ -48,11 +48,12 @@ struct ag_q8_meta {
 hipError_t ag_launch_rotate(ag_ctx *ctx, hipStream_t s, const void *q, const void *k, ag_dtype dt, int B, int Hq, int Hkv, int L,
                             int D, const ag_rope_dev &rope, void *q_out, void *k_out);
 
-// Appends the kept tokens.  words, blk_off (nullptr: every token is kept): the flags' masks and prefix counts (ag_launch_flag_scan).
+// Appends the tokens whose flag is set (flags == nullptr: all).  words, blk_off: where the flags' masks and prefix counts go (as from
+// ag_launch_flag_scan; not used without flags).
 // tiles != nullptr: also leaves, for the attention, [units, n_blk] tiles of 64 rows of K (turned) and V -- the tail's rows as they stood, then
 // the appended ones -- with what they are to be read with (q8_tile_info), and meta [units].
-hipError_t ag_launch_q8_fill(ag_ctx *ctx, hipStream_t s, const void *k, const void *v, int B, int Hkv, int L, int D,
-                             const uint64_t *words, const int32_t *blk_off, const ag_rope_dev &rope, const ag_q8_dev &cache,
+hipError_t ag_launch_q8_fill(ag_ctx *ctx, hipStream_t s, const void *k, const void *v, const uint8_t *flags, int B, int Hkv, int L, int D,
+                             uint64_t *words, int32_t *blk_off, const ag_rope_dev &rope, const ag_q8_dev &cache,
                              uint16_t *tiles, uint32_t *info, ag_q8_meta *meta);
 size_t ag_ws_q8_decode_floats(int num_cu, int G, int D);  // records of a step
 hipError_t ag_launch_q8_decode(ag_ctx *ctx, hipStream_t s, const void *q, const void *k_new, const void *v_new, const uint8_t *new_flags,

@@ -130,8 +130,7 @@ ag_status ag_q8_append(ag_ctx *ctx, void *hip_stream, const void *k, const void 
   st = ag_need_device(ctx);
   if (st != AG_OK) return st;
   hipStream_t s = (hipStream_t)hip_stream;
-  if (flags) AG_HIP(ag_launch_flag_scan(ctx, s, flags, units, L, scan.words, scan.blk_off, nullptr));
-  AG_HIP(ag_launch_q8_fill(ctx, s, k, v, cache->B, cache->Hkv, L, cache->D, scan.words, scan.blk_off, r, c, nullptr, nullptr, nullptr));
+  AG_HIP(ag_launch_q8_fill(ctx, s, k, v, flags, cache->B, cache->Hkv, L, cache->D, scan.words, scan.blk_off, r, c, nullptr, nullptr, nullptr));
   return AG_OK;
 }
 
@@ -161,8 +160,7 @@ ag_status ag_q8_prefill_attn(ag_ctx *ctx, void *hip_stream, const void *q, const
   st = ag_need_device(ctx);
   if (st != AG_OK) return st;
   hipStream_t s = (hipStream_t)hip_stream;
-  if (flags) AG_HIP(ag_launch_flag_scan(ctx, s, flags, units, L, scan.words, scan.blk_off, nullptr));
-  AG_HIP(ag_launch_q8_fill(ctx, s, k, v, cache->B, cache->Hkv, L, cache->D, scan.words, scan.blk_off, r, c, w.tiles, w.info, w.meta));
+  AG_HIP(ag_launch_q8_fill(ctx, s, k, v, flags, cache->B, cache->Hkv, L, cache->D, scan.words, scan.blk_off, r, c, w.tiles, w.info, w.meta));
   AG_HIP(ag_launch_q8_prefill(ctx, s, q, k, v, cache->B, Hq, cache->Hkv, L, cache->D, scan.words, scan.blk_off, r, scale, c, w, out));
   return AG_OK;
 }

@@ -23,7 +23,10 @@
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int NW = 8, NT = 64 * NW;
+// Up to here 8 waves per workgroup and one workgroup per CU: a unit's items are spread over as many waves as the registers allow;
+// beyond, 4 waves and two workgroups per CU, so that one streams while the other starts or merges.
+constexpr int kFewUnits = 128;
+constexpr int kWholeRounds = 2;   // items of a wave up to which a unit is not cut: the meeting of the pieces costs as much as a round
 constexpr int kArriveSplit = 64;  // workgroups from which their arrivals are counted at several addresses
 constexpr int kTeamRounds = 6;    // items of a wave up to which units are given to teams of waves
 
@@ -60,6 +63,18 @@ __device__ __forceinline__ int wave_prefix(int x, int &total) {
   total = __builtin_amdgcn_readlane(y, 63);
   return y - x;
 }
+// Over the wave's lanes (register exchanges: no addresses that live in registers, as lane shuffles have them)
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+  auto dpp = [](uint32_t y, auto ctrl) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)y, decltype(ctrl)::value, 0xf, 0xf, false); };
+  x = max(x, dpp(x, std::integral_constant<int, 0xB1>{}));   // quad_perm [1,0,3,2]
+  x = max(x, dpp(x, std::integral_constant<int, 0x4E>{}));   // quad_perm [2,3,0,1]
+  x = max(x, dpp(x, std::integral_constant<int, 0x141>{}));  // row_half_mirror
+  x = max(x, dpp(x, std::integral_constant<int, 0x140>{}));  // row_mirror
+  const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  x = max((uint32_t)a[0], (uint32_t)a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return __builtin_amdgcn_readfirstlane(max((uint32_t)b[0], (uint32_t)b[1]));
+}
 // Over the four lanes that share lane % 16
 __device__ __forceinline__ float kg_max(float x) {
   const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -80,72 +95,73 @@ template <int N> __device__ __forceinline__ float column(float x) {
 
 template <int D, int G> struct wave_q8 {
   static constexpr int KC = D / 64, KF = 4 * KC, VF = D / 16;
-  static constexpr int P = G <= 4 ? 4 : 8, PARTS = P == 4 ? 3 : 2;
+  static constexpr int P = G <= 4 ? 4 : 8;
   static constexpr int SF = D + 4;  // floats per head of the state a wave leaves: max, sum, -, -, o
-  q8_bf16x8 qf[KC][2][2];
+  q8_f16x8 qf[KC][2];
+  int eq;                           // qf: the query times 2^-eq
   q8_f32x4 o[VF];
   float m, l;
-  int lane, g, col, head, part;
+  int lane, g, col, head;
+  bool second;                      // (columns P and up: what a weight of the tail leaves over)
 
   __device__ __forceinline__ void init(int lane_) {
-    lane = lane_; g = lane >> 4; col = lane & 15; head = col % P; part = col / P;
-    m = kQ8EmptyMax; l = 0.f;
+    lane = lane_; g = lane >> 4; col = lane & 15; head = col % P; second = col >= P;
+    m = kQ8EmptyMax; l = 0.f; eq = 0;
 #pragma unroll
     for (int f = 0; f < VF; ++f) o[f] = q8_f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  // This lane's 16 values of each 64 columns of a vector, turned by the token's angles (in LDS: cosines, sines).
-  __device__ __forceinline__ void vector(q8_eight (&y)[KC][2], const uint16_t *x, const float *angles) {
-    uint4 raw[KC][2];
+  // This lane's 16 values of each 64 columns of a vector: as they lie in memory, then turned by the token's angles (in LDS:
+  // cosines, sines).
+  struct raw_t {
+    uint4 x[KC][2], p[KC == 2 ? 1 : 2];  // (KC = 1: the partners belong to another lane)
+  };
+  __device__ __forceinline__ raw_t fetch(const uint16_t *x) const {
+    raw_t r;
+#pragma unroll
+    for (int c = 0; c < KC; ++c)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) r.x[c][s] = *reinterpret_cast<const uint4 *>(x + 64 * c + 16 * g + 8 * s);
+    if constexpr (KC == 1) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s) r.p[s] = *reinterpret_cast<const uint4 *>(x + ((16 * g + 8 * s) ^ (D / 2)));
+    }
+    return r;
+  }
+  __device__ __forceinline__ void vector(q8_eight (&y)[KC][2], const raw_t &r, const float *angles) const {
 #pragma unroll
     for (int c = 0; c < KC; ++c)
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        raw[c][s] = *reinterpret_cast<const uint4 *>(x + 64 * c + 16 * g + 8 * s);
-        y[c][s] = q8_floats(raw[c][s]);
-      }
-    if (angles) {
-#pragma unroll
-      for (int c = 0; c < KC; ++c)
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          uint4 p;
-          if constexpr (KC == 2) p = raw[c ^ 1][s];
-          else p = *reinterpret_cast<const uint4 *>(x + ((16 * g + 8 * s) ^ (D / 2)));
-          y[c][s] = q8_turn8<D>(
-              [&](int i) { return q8_angles{*reinterpret_cast<const float4 *>(angles + i), *reinterpret_cast<const float4 *>(angles + D / 2 + i)}; },
-              64 * c + 16 * g + 8 * s, raw[c][s], p);
+        if (!angles) {
+          y[c][s] = q8_floats(r.x[c][s]);
+          continue;
         }
-    }
+        uint4 p;
+        if constexpr (KC == 2) p = r.x[c ^ 1][s];
+        else p = r.p[s];
+        y[c][s] = q8_turn8<D>(
+            [&](int i) { return q8_angles{*reinterpret_cast<const float4 *>(angles + i), *reinterpret_cast<const float4 *>(angles + D / 2 + i)}; },
+            64 * c + 16 * g + 8 * s, r.x[c][s], p);
+      }
   }
-  // The query as two bf16 numbers a value: a turned one rounded to the first alone would shift the scores by 2^-9 of their size.
-  __device__ __forceinline__ void query(const uint16_t *q, const float *angles) {
+  // The query in f16 (11 bits: a turned one in bf16 would shift the scores by 2^-9 of their size), its largest value in [2^14, 2^15)
+  __device__ __forceinline__ void query(const raw_t &r, const float *angles) {
     q8_eight y[KC][2];
-    vector(y, q + (size_t)min(head, G - 1) * D, angles);
+    vector(y, r, angles);
+    float top = 0.f;
+#pragma unroll
+    for (int c = 0; c < KC; ++c) top = fmaxf(top, fmaxf(y[c][0].top(), y[c][1].top()));
+    top = kg_max(top);
+    eq = max(kQ8TileMinExp, min(254, max(1, (int)(__float_as_uint(top) >> 23))) - 127 - kQ8TileTop);
+    const float inv = q8_pow2(-eq);
 #pragma unroll
     for (int c = 0; c < KC; ++c)
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        const uint4 hi = y[c][s].bf16();
-        const q8_eight h = q8_floats(hi);
-        qf[c][s][0] = __builtin_bit_cast(q8_bf16x8, hi);
-        qf[c][s][1] = __builtin_bit_cast(q8_bf16x8, q8_eight{y[c][s].a - h.a, y[c][s].b - h.b}.bf16());
-      }
+      for (int s = 0; s < 2; ++s) qf[c][s] = y[c][s].f16(inv);
   }
-  // Scores of 16 rows with 32 columns of each step: sums of the two parts apart, and added at the end.
-  __device__ __forceinline__ void score(q8_f32x4 (&x)[2], int c, int h, const q8_bf16x8 &k) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) x[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qf[c][h][i], x[i], 0, 0, 0);
-  }
-  // The weights of 64 rows from their scores (score(a): rows 16 a + 4 g + 0..3), then O += p V (value(f, i): columns 16 f .., rows 32 i ..).
-  template <typename VAL>
-  __device__ __forceinline__ void weigh(q8_f32x4 (&s)[4], float qscale, VAL &&value) {
-    float p[16], mx = -INFINITY;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      p[e] = s[e >> 2][e & 3] * qscale;
-      mx = fmaxf(mx, p[e]);
-    }
-    const float m_new = fmaxf(m, kg_max(mx));
+
+  // A new reference for the scores (their tile's exponent included): everything so far shrinks to it.
+  __device__ __forceinline__ void raise(float m_new) {
     if (__any(m_new != m)) {
       const float alpha = __builtin_amdgcn_exp2f(m - m_new);
       l *= alpha;
@@ -153,82 +169,103 @@ template <int D, int G> struct wave_q8 {
       for (int f = 0; f < VF; ++f) o[f] *= alpha;
       m = m_new;
     }
-    // Part 0 is the first 16 bits of a number just below p, part 1 those of a number just below what is left, the last part what is left
-    // then (two parts: rounded): all of them are positive where p is not 0, so that an infinite value comes out with its sign.
-    uint32_t w[8];
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      p[e] = __builtin_amdgcn_exp2f(p[e] - m);
-      l += p[e];
-      const uint32_t w0 = __builtin_elementwise_sub_sat(__float_as_uint(p[e]), 1u) & 0xffff0000u;
-      const float r1 = p[e] - __uint_as_float(w0);
-      if constexpr (PARTS == 3) {
-        const uint32_t w1 = __builtin_elementwise_sub_sat(__float_as_uint(r1), 1u) & 0xffff0000u;
-        const float r2 = r1 - __uint_as_float(w1);
-        p[e] = __uint_as_float(part == 0 ? w0 : part == 1 ? w1 : part == 2 ? __float_as_uint(r2) : 0u);
-      } else {
-        p[e] = part == 0 ? __uint_as_float(w0) : r1;
-      }
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) w[e] = q8_pack2(p[2 * e], p[2 * e + 1]);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const q8_bf16x8 pb = __builtin_bit_cast(q8_bf16x8, make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));
-#pragma unroll
-      for (int f = 0; f < VF; ++f) o[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(value(f, i), pb, o[f], 0, 0, 0);
-    }
   }
 
-  // Pages i0, i0 + step, ... < i1 of a unit.
-  __device__ __forceinline__ void pages(const ag_q8_dev &c, const int32_t *page, int i0, int i1, int step, float qscale) {
-    q8_u32x4 kr[KF], vr[VF];
-    float ks = 1.f, vs = 1.f, ks_next = 1.f, vs_next = 1.f;
-    auto id_of = [&](int i) { return __builtin_amdgcn_readfirstlane(page[i]); };
-    auto there = [&](int p) { return (unsigned)p < (unsigned)c.n_pages; };
-    auto load = [&](const uint8_t *pool, int p, auto &r) {  // every page is read once per step: non-temporal
-      const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)(pool + (size_t)p * (kQ8Block * D)), 0, kQ8Block * D, 0x00020000);
+  // Pages i0, i0 + step, ... < i1 of a unit: the first one is asked for before the query is there.
+  q8_u32x4 kr[KF], vr[VF];
+  float ks, vs;
+  int next;
+  bool ok;
+  __device__ __forceinline__ int id_of(const int32_t *page, int i) const { return __builtin_amdgcn_readfirstlane(page[i]); }
+  template <typename R> __device__ __forceinline__ void load(const uint8_t *pool, int p, R &r) const {  // every page is read once per step: non-temporal
+    const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)(pool + (size_t)p * (kQ8Block * D)), 0, kQ8Block * D, 0x00020000);
 #pragma unroll
-      for (int f = 0; f < (int)(sizeof(r) / sizeof(r[0])); ++f) r[f] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, lane * 16 + (f & 3) * 1024, f / 4 * 4096, 2);
-    };
-    if (i0 >= i1) return;
-    int id = id_of(i0), next = i0 + step < i1 ? id_of(i0 + step) : 0;
-    bool ok = there(id);
+    for (int f = 0; f < (int)(sizeof(R) / sizeof(r[0])); ++f) r[f] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, lane * 16 + (f & 3) * 1024, f / 4 * 4096, 2);
+  }
+  __device__ __forceinline__ void first_page(const ag_q8_dev &c, int id, int id_next) {
+    next = id_next;
+    ok = (uint32_t)id < (uint32_t)c.n_pages;
     if (!ok) id = 0;
     load(c.k, id, kr);
     load(c.v, id, vr);
     ks = c.k_scale[id]; vs = c.v_scale[id];
+  }
+  // The state is kept relative to m, the largest score plus its page's exponent ev of V: a page's weights are 2^(score + ev - m) in f16, its values
+  // the codes, and its part of the row sum is 2^-ev the sum of its weights.
+  __device__ __forceinline__ void pages(const ag_q8_dev &c, const int32_t *page, int i0, int i1, int step, float qscale) {
+    float ks_next = 1.f, vs_next = 1.f;
+    bool fresh = true;
     for (int i = i0; i < i1; i += step) {
       const bool more = i + step < i1, now = ok;
-      id = next;
+      int id = next;
       if (more) {
-        ok = there(id);
+        ok = (uint32_t)id < (uint32_t)c.n_pages;
         if (!ok) id = 0;
-        next = i + 2 * step < i1 ? id_of(i + 2 * step) : 0;
+        next = i + 2 * step < i1 ? id_of(page, i + 2 * step) : 0;
         ks_next = c.k_scale[id]; vs_next = c.v_scale[id];
       }
       q8_f32x4 s[4];
 #pragma unroll
       for (int a = 0; a < 4; ++a) {
-        q8_f32x4 x[2] = {q8_f32x4{0.f, 0.f, 0.f, 0.f}, q8_f32x4{0.f, 0.f, 0.f, 0.f}};
+        s[a] = q8_f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int cc = 0; cc < KC; ++cc)
 #pragma unroll
-          for (int h = 0; h < 2; ++h) score(x, cc, h, q8_widen(kr[a * KC + cc][2 * h], kr[a * KC + cc][2 * h + 1], ks));
-        s[a] = x[0] + x[1];
+          for (int h = 0; h < 2; ++h)
+            s[a] = __builtin_amdgcn_mfma_f32_16x16x32_f16(q8_widen16(kr[a * KC + cc][2 * h], kr[a * KC + cc][2 * h + 1], 1.f), qf[cc][h], s[a], 0, 0, 0);
       }
       if (more) load(c.k, id, kr);
-      if (!now) {  // (a page id outside the pool: rows that are not there)
+      if (now) {  // (a page number outside the pool: rows that are not there)
+        auto exponent = [](float x) { return (int)(__builtin_amdgcn_readfirstlane(__float_as_uint(x)) >> 23) - 127; };
+        const int e = exponent(vs), ev = max(kQ8TileMinExp, e);
+        const float f = fmaxf(ldexpf(qscale, eq + exponent(ks)), 1.17549435e-38f);
+        float sum;
+        uint32_t w[8];
+        auto largest = [&] {
+          float mx = s[0][0];
 #pragma unroll
-        for (int a = 0; a < 4; ++a) s[a] = q8_f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          for (int x = 1; x < 16; ++x) mx = fmaxf(mx, s[x >> 2][x & 3]);
+          return fmaxf(m, fmaf(kg_max(mx), f, (float)ev));
+        };
+        auto weigh = [&] {
+          const float off = (float)ev - m;
+          sum = 0.f;
+#pragma unroll
+          for (int x = 0; x < 8; ++x) {
+            const q8_f32x2 p = {__builtin_amdgcn_exp2f(fmaf(s[x >> 1][2 * (x & 1)], f, off)), __builtin_amdgcn_exp2f(fmaf(s[x >> 1][2 * (x & 1) + 1], f, off))};
+            sum += p[0] + p[1];
+            w[x] = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, q8_f16x2));
+          }
+        };
+        if (fresh) raise(largest());
+        fresh = false;
+        weigh();
+        // no maximum in the common case: only where weights pass 2^15 is the reference moved (for that head alone)
+        if (__any(!(sum <= 32768.f))) {
+          const float m_new = largest();
+          raise(kg_max(sum <= 32768.f ? 0.f : 1.f) > 0.f ? m_new : m);
+          weigh();
+        }
+        l += ldexpf(sum, -ev);
+        const float scale = q8_pow2(e - ev);
+#pragma unroll
+        for (int x = 0; x < 8; ++x) w[x] = second ? 0u : w[x];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const q8_f16x8 pb = __builtin_bit_cast(q8_f16x8, make_uint4(w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3]));
+#pragma unroll
+          for (int x = 0; x < VF; ++x)
+            o[x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(q8_widen16(vr[x][2 * h], vr[x][2 * h + 1], scale), pb, o[x], 0, 0, 0);
+        }
       }
-      weigh(s, qscale, [&](int f, int h) { return q8_widen(vr[f][2 * h], vr[f][2 * h + 1], now ? vs : 1.f); });
       if (more) load(c.v, id, vr);
       ks = ks_next; vs = vs_next;
     }
   }
 
-  // The tail's n rows and the new token as row n (nk: this lane's part of its turned key); `append`: the new row stays.
+  // The tail's n rows and the new token as row n (nk: this lane's part of its turned key); `append`: the new row stays.  The rows are bf16
+  // of any size, so these products are in bf16: the query and the weights as the sum of two numbers each (the weights' second one
+  // in the columns P further, which are idle otherwise).
   __device__ __forceinline__ void tail(const dec_args &a, int u, int n, int block, bool append, const uint4 (&nk)[KC][2]) {
     uint16_t *kt = a.c.k_tail + (size_t)u * kQ8Block * D, *vt = a.c.v_tail + (size_t)u * kQ8Block * D;
     const uint16_t *vn = a.v_new + (size_t)u * D;
@@ -249,9 +286,9 @@ template <int D, int G> struct wave_q8 {
     for (int f = 0; f < VF; ++f)
 #pragma unroll
       for (int i = 0; i < 2; ++i) vr[f][i] = load(v_rsrc, (f * 64 + lane) * 32 + 16 * i, 32 * i + 4 * g < n);
-    uint16_t nv[VF];
+    uint32_t nv[VF / 2];  // this lane's values of the new token, two a register
 #pragma unroll
-    for (int f = 0; f < VF; ++f) nv[f] = vn[16 * f + col];
+    for (int f = 0; f < VF / 2; ++f) nv[f] = (uint32_t)vn[32 * f + col] | (uint32_t)vn[32 * f + 16 + col] << 16;
     // the new row joins: row n = 16 (n / 16) + col for K, = 16 i + 4 g + n % 4 for V
 #pragma unroll
     for (int x = 0; x < 4; ++x)
@@ -270,28 +307,38 @@ template <int D, int G> struct wave_q8 {
     }
     q8_f32x4 s[4];
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      q8_f32x4 y[2] = {q8_f32x4{0.f, 0.f, 0.f, 0.f}, q8_f32x4{0.f, 0.f, 0.f, 0.f}};
+    for (int x = 0; x < 4; ++x) s[x] = q8_f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int c = 0; c < KC; ++c)
+    for (int c = 0; c < KC; ++c)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) score(y, c, h, __builtin_bit_cast(q8_bf16x8, kr[x][c][h]));
-      s[x] = y[0] + y[1];
+      for (int h = 0; h < 2; ++h) {
+        const q8_f16x8 q = qf[c][h];
+        const q8_eight y = {{(float)q[0], (float)q[1], (float)q[2], (float)q[3]}, {(float)q[4], (float)q[5], (float)q[6], (float)q[7]}};
+        const uint4 hi = y.bf16();
+        const q8_eight z = q8_floats(hi);
+        const q8_bf16x8 qh = __builtin_bit_cast(q8_bf16x8, hi), ql = __builtin_bit_cast(q8_bf16x8, q8_eight{y.a - z.a, y.b - z.b}.bf16());
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const q8_bf16x8 k = __builtin_bit_cast(q8_bf16x8, kr[x][c][h]);
+          s[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, ql, s[x], 0, 0, 0);
+          s[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qh, s[x], 0, 0, 0);
+        }
+      }
+    const float f = fmaxf(ldexpf(a.qscale, eq), 1.17549435e-38f);
+    float mx = -INFINITY;
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int row = 16 * x + 4 * g + r;
+        s[x][r] *= f;
         if (row > n) s[x][r] = -INFINITY;
         // the new token: alone its weight is 1 whatever its score is; a score that overflowed to -infinity counts as the least number
-        if (row == n) s[x][r] = n == 0 && block == 0 ? 0.f : (s[x][r] == -INFINITY ? kQ8EmptyMax : s[x][r]);
+        if (row == n) s[x][r] = n == 0 && block == 0 ? 0.f : (s[x][r] < kQ8EmptyMax ? kQ8EmptyMax : s[x][r]);
+        mx = fmaxf(mx, s[x][r]);
       }
-    }
     auto narrow = [](const uint4 &x, const uint4 &y, float inv) {
       return make_uint4(q8_narrow(x.x, x.y, inv), q8_narrow(x.z, x.w, inv), q8_narrow(y.x, y.y, inv), q8_narrow(y.z, y.w, inv));
-    };
-    auto wave_max = [](uint32_t top) {
-#pragma unroll
-      for (int x = 32; x > 0; x >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, x, 64));
-      return q8_exponent(__builtin_amdgcn_readfirstlane(top));
     };
     auto top4 = [](uint32_t top, const uint4 &w) { return q8_top(q8_top(q8_top(q8_top(top, w.x), w.y), w.z), w.w); };
     const int id = fills ? a.c.page[(size_t)u * a.c.max_blocks + block] : 0;
@@ -301,7 +348,7 @@ template <int D, int G> struct wave_q8 {
       for (int x = 0; x < 4; ++x)
 #pragma unroll
         for (int c = 0; c < KC; ++c) top = top4(top4(top, kr[x][c][0]), kr[x][c][1]);
-      const int e = wave_max(top);
+      const int e = q8_exponent(wave_max(top));
       const float inv = q8_pow2(-e);
       uint4 *to = reinterpret_cast<uint4 *>(a.c.k + (size_t)id * kQ8Block * D) + lane;
 #pragma unroll
@@ -309,6 +356,22 @@ template <int D, int G> struct wave_q8 {
 #pragma unroll
         for (int c = 0; c < KC; ++c) to[(x * KC + c) * 64] = narrow(kr[x][c][0], kr[x][c][1], inv);
       if (lane == 0) a.c.k_scale[id] = q8_pow2(e);
+    }
+    raise(fmaxf(m, kg_max(mx)));
+    // A weight's first part is the first 16 bits of a number just below it, its second one what is left, rounded: both are positive
+    // where the weight is not 0, so that an infinite value comes out with its sign.
+    uint32_t w[8];
+#pragma unroll
+    for (int x = 0; x < 16; x += 2) {
+      float p[2];
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        p[y] = __builtin_amdgcn_exp2f(s[x >> 2][(x & 3) + y] - m);
+        l += p[y];
+        const float first = __uint_as_float(__builtin_elementwise_sub_sat(__float_as_uint(p[y]), 1u) & 0xffff0000u);
+        p[y] = second ? p[y] - first : first;
+      }
+      w[x / 2] = q8_pack2(p[0], p[1]);
     }
     uint32_t old[8], mine[8];  // halves of word y (rows 16 (y / 2) + 4 g + 2 (y % 2) + 0, 1) that are rows before n, and row n
 #pragma unroll
@@ -319,26 +382,27 @@ template <int D, int G> struct wave_q8 {
     }
 #pragma unroll
     for (int f = 0; f < VF; ++f) {
-      const uint32_t two = (uint32_t)nv[f] * 0x10001u;
+      const uint32_t two = __builtin_amdgcn_perm(nv[f / 2], nv[f / 2], f & 1 ? 0x07060706u : 0x05040504u);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        uint4 &w = vr[f][i];
-        w.x = (w.x & old[4 * i]) | (two & mine[4 * i]);
-        w.y = (w.y & old[4 * i + 1]) | (two & mine[4 * i + 1]);
-        w.z = (w.z & old[4 * i + 2]) | (two & mine[4 * i + 2]);
-        w.w = (w.w & old[4 * i + 3]) | (two & mine[4 * i + 3]);
+        uint4 &v = vr[f][i];
+        v.x = (v.x & old[4 * i]) | (two & mine[4 * i]);
+        v.y = (v.y & old[4 * i + 1]) | (two & mine[4 * i + 1]);
+        v.z = (v.z & old[4 * i + 2]) | (two & mine[4 * i + 2]);
+        v.w = (v.w & old[4 * i + 3]) | (two & mine[4 * i + 3]);
+        o[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(q8_bf16x8, v),
+                                                       __builtin_bit_cast(q8_bf16x8, make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3])), o[f], 0, 0, 0);
       }
     }
     if (append && !fills && g == ((n >> 2) & 3)) {
 #pragma unroll
-      for (int f = 0; f < VF; ++f) vt[(f * 64 + lane) * 16 + (n >> 4) * 4 + (n & 3)] = nv[f];
+      for (int f = 0; f < VF; ++f) vt[(f * 64 + lane) * 16 + (n >> 4) * 4 + (n & 3)] = (uint16_t)(nv[f / 2] >> (16 * (f & 1)));
     }
-    weigh(s, a.qscale, [&](int f, int i) { return __builtin_bit_cast(q8_bf16x8, vr[f][i]); });
     if (fills) {
       uint32_t top = 0;
 #pragma unroll
       for (int f = 0; f < VF; ++f) top = top4(top4(top, vr[f][0]), vr[f][1]);
-      const int e = wave_max(top);
+      const int e = q8_exponent(wave_max(top));
       const float inv = q8_pow2(-e);
       uint4 *to = reinterpret_cast<uint4 *>(a.c.v + (size_t)id * kQ8Block * D) + lane;
 #pragma unroll
@@ -354,7 +418,7 @@ template <int D, int G> struct wave_q8 {
       q8_f32x4 x;
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        x[r] = P == 4 ? o[f][r] + column<4>(o[f][r]) + column<8>(o[f][r]) : o[f][r] + column<8>(o[f][r]);
+        x[r] = o[f][r] + column<P>(o[f][r]);
       if (col < G) *reinterpret_cast<q8_f32x4 *>(st + col * SF + 4 + 16 * f + 4 * g) = x;
     }
     if (col < G && g == 0) {
@@ -364,101 +428,132 @@ template <int D, int G> struct wave_q8 {
   }
 };
 
-template <int D, int G>
-__global__ __launch_bounds__(NT, 2) void ag_q8_decode_kernel(dec_args a) {
+template <int D, int G, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void ag_q8_decode_kernel(dec_args a) {
+  constexpr int NT = 64 * NW;
   typedef wave_q8<D, G> wave_t;
   constexpr int SF = wave_t::SF;
+  constexpr bool kRegs = NW == 8;  // the work list lives in registers
   __shared__ __attribute__((aligned(16))) float s_state[NW][G * SF];
   __shared__ __attribute__((aligned(16))) float s_angles[NW][D];
   extern __shared__ int32_t s_len[];  // [U] rows held; top bit: another one fits
-  __shared__ int32_t w_sum[NW][4], s_start[2], s_last, s_order;
+  __shared__ int32_t w_sum[NW][2], s_start[2], s_last, s_order;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int U = a.U, wg = blockIdx.x, grid = gridDim.x;
   const int most = a.c.max_blocks * kQ8Block + kQ8Block - 1;
 
+  // The arguments lie in several cache lines of memory: all are asked for here, not one after the other as the code comes to need them.
+  asm volatile("" :: "s"(a.q), "s"(a.out), "s"(a.c.len), "s"(a.c.n_pages), "s"(a.rope.n_rows), "s"(a.U));
   // ---- the work list ----
   auto items_of = [](int n) { return (n & 0x7fffffff) / kQ8Block + 1; };
-  const int per = (U + NT - 1) / NT, u0 = min(U, tid * per), u1 = min(U, u0 + per);  // this thread's units
-  int my_t = 0, max_t = 0;
-  for (int v = u0; v < u1; ++v) {
-    int n = max(0, min(a.c.len[v], most));
-    const int at = n / kQ8Block;
-    if ((n & (kQ8Block - 1)) != kQ8Block - 1 ||
-        (at < a.c.max_blocks && (unsigned)a.c.page[(size_t)v * a.c.max_blocks + at] < (unsigned)a.c.n_pages))
-      n |= (int)0x80000000;
-    s_len[v] = n;
-    my_t += items_of(n);
-    max_t = max(max_t, items_of(n));
-  }
-  int sum;
-  int pre_t = wave_prefix(my_t, sum);
-  for (int x = 32; x > 0; x >>= 1) max_t = max(max_t, __shfl_xor(max_t, x, 64));
-  if (lane == 0) { w_sum[wave][0] = sum; w_sum[wave][1] = max_t; }
-  __syncthreads();
-  // The lengths may only change once every workgroup has read them: each counts its arrival, the last one writes them at its end.
-  const int groups = grid >= kArriveSplit ? kDecodeArriveGroups : 1;
-  if (tid == 0)
+  int piece = NW;                                       // items of a piece: rounds of the workgroup's waves
+  uint32_t piece_inv = (uint32_t)((1ull << 32) / NW);   // ceil(2^32 / piece): x / piece for x piece < 2^32
+  auto pieces_of = [&](int t) { return t <= max(kWholeRounds * NW, piece) ? 1 : (int)__umulhi((uint32_t)(t + piece - 1), piece_inv); };
+  auto set_rounds = [&](int r) {
+    piece = r * NW;
+    piece_inv = 0xffffffffu / (uint32_t)piece + 1u;
+  };
+  auto read_len = [&](int v) {  // rows of unit v, top bit set if another one fits
+    const int n = max(0, min(a.c.len[v], most)), at = n / kQ8Block;
+    bool room = (n & (kQ8Block - 1)) != kQ8Block - 1;
+    if (!room) room = at < a.c.max_blocks && (uint32_t)a.c.page[(size_t)v * a.c.max_blocks + min(at, a.c.max_blocks - 1)] < (uint32_t)a.c.n_pages;
+    return n | (room ? (int)0x80000000 : 0);
+  };
+  // The lengths may only change once every workgroup has read them: each counts its arrival when it has (8 waves: at its end), and the
+  // one that arrives last writes them.
+  const int groups = !kRegs && grid >= kArriveSplit ? kDecodeArriveGroups : 1;
+  auto arrive = [&] {
     s_order = __hip_atomic_fetch_add(a.arrived + (groups == 1 ? 0 : kDecodeArriveStride * (1 + wg % kDecodeArriveGroups)), 1, __ATOMIC_RELAXED,
-                                   __HIP_MEMORY_SCOPE_AGENT);
-  int total = 0;
-  max_t = 0;
+                                     __HIP_MEMORY_SCOPE_AGENT);
+  };
+  int sl_r[2] = {0, 0};                                                              // kRegs: this lane's units, lane and 64 + lane
+  const int per = (U + NT - 1) / NT, u0 = min(U, tid * per), u1 = min(U, u0 + per);  // else this thread's
+  int total = 0, u = 0, sub = 0, team = NW, quota = 0, x = 0;
+  bool by_piece = false, by_team = false, idle;
+  if constexpr (kRegs) {  // (at most kFewUnits units: every wave by itself, without LDS and barriers)
+    int t[2] = {0, 0}, pre_t[2], pre_p[2] = {0, 0}, p[2] = {0, 0}, pieces = 0, sum;
 #pragma unroll
-  for (int w = 0; w < NW; ++w) {
-    if (w < wave) pre_t += w_sum[w][0];
-    total += w_sum[w][0];
-    max_t = max(max_t, w_sum[w][1]);
-  }
-  // pieces of `piece` items: the fewest rounds of the waves for which every piece has a workgroup (sure for r2 rounds, where U < grid)
-  const int r1 = max(1, (total + NW * grid - 1) / (NW * grid)), r2 = U < grid ? max(r1, (total + NW * (grid - U) - 1) / (NW * (grid - U))) : 0;
-  auto pieces_of = [](int t, int piece) { return (t + piece - 1) / piece; };
-  int my_1 = 0, my_2 = 0;
-  if (U < grid)
-    for (int v = u0; v < u1; ++v) {
-      my_1 += pieces_of(items_of(s_len[v]), r1 * NW);
-      my_2 += pieces_of(items_of(s_len[v]), r2 * NW);
+    for (int j = 0; j < 2; ++j)
+      if (64 * j + lane < U) sl_r[j] = read_len(64 * j + lane);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      if (64 * j + lane < U) t[j] = items_of(sl_r[j]);
+      pre_t[j] = total + wave_prefix(t[j], sum);
+      total += sum;
     }
-  int sum_1, sum_2;
-  int pre_1 = wave_prefix(my_1, sum_1), pre_2 = wave_prefix(my_2, sum_2);
-  if (lane == 0) { w_sum[wave][2] = sum_1; w_sum[wave][3] = sum_2; }
-  __syncthreads();
-  int all_1 = 0, all_2 = 0;
+    // pieces of the fewest rounds of the waves for which every piece has a workgroup (sure for the second try)
+    int rounds = 1;
+    if (total > NW * grid) rounds = (int)((uint32_t)(total + NW * grid - 1) / (uint32_t)(NW * grid));
+    for (bool last = false;; last = true) {
+      if (rounds > 1) set_rounds(rounds);
+      pieces = 0;
 #pragma unroll
-  for (int w = 0; w < NW; ++w) {
-    if (w < wave) { pre_1 += w_sum[w][2]; pre_2 += w_sum[w][3]; }
-    all_1 += w_sum[w][2];
-    all_2 += w_sum[w][3];
-  }
-  const bool by_1 = U < grid && all_1 <= grid;
-  const int rounds = by_1 ? r1 : r2, piece = rounds * NW;
-  // ... unless so many units are cut that the remainders of their last pieces weigh more than equal ranges cost
-  const bool by_piece = U < grid && (rounds <= 2 || 4 * U <= grid);
-  int team = NW;
-  while (team > 1 && U * team > grid * NW) team /= 2;
-  const bool by_team = !by_piece && U * team <= grid * NW && max_t <= kTeamRounds * team;
-  const int quota = (total + grid - 1) / grid;
-  int u = 0, sub = 0;
-  bool idle;
-  const int x = by_piece ? wg : wg * quota;
-  if (by_team) {
-    u = wg * (NW / team) + wave / team;
-    idle = wg * (NW / team) >= U;
-  } else {
-    team = NW;
-    idle = x >= (by_piece ? (by_1 ? all_1 : all_2) : total);
-    int at = by_piece ? (by_1 ? pre_1 : pre_2) : pre_t;
-    const int mine = by_piece ? (by_1 ? my_1 : my_2) : my_t;
-    if (at <= x && x < at + mine) {  // exactly one thread, if there is one
-      int v = u0;
-      for (;; ++v) {
-        const int t = by_piece ? pieces_of(items_of(s_len[v]), piece) : items_of(s_len[v]);
-        if (x < at + t) break;
-        at += t;
+      for (int j = 0; j < 2; ++j) {
+        p[j] = t[j] ? pieces_of(t[j]) : 0;
+        pre_p[j] = pieces + wave_prefix(p[j], sum);
+        pieces += sum;
       }
-      s_start[0] = v;
-      s_start[1] = x - at;
+      if (pieces <= grid || last || U >= grid) break;
+      rounds = max(rounds, (int)((uint32_t)(total + NW * (grid - U) - 1) / (uint32_t)(NW * (grid - U))));
     }
+    // ... unless so many units are cut that the remainders of their last pieces weigh more than equal ranges cost
+    by_piece = pieces <= grid && (rounds <= 2 || 4 * U <= grid);
+    if (!by_piece) quota = (int)((uint32_t)(total + grid - 1) / (uint32_t)grid);
+    x = by_piece ? wg : wg * quota;
+    idle = x >= (by_piece ? pieces : total);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int from = by_piece ? pre_p[j] : pre_t[j], n = by_piece ? p[j] : t[j];
+      const uint64_t hit = __ballot(from <= x && x < from + n);
+      if (hit) {
+        const int at = __builtin_ctzll(hit);
+        u = 64 * j + at;
+        sub = x - __builtin_amdgcn_readlane(from, at);
+      }
+    }
+  } else {
+    int my_t = 0, max_t = 0, sum;
+    for (int v = u0; v < u1; ++v) {
+      const int n = read_len(v);
+      s_len[v] = n;
+      my_t += items_of(n);
+      max_t = max(max_t, items_of(n));
+    }
+    int pre_t = wave_prefix(my_t, sum);
+    max_t = (int)wave_max((uint32_t)max_t);
+    if (lane == 0) { w_sum[wave][0] = sum; w_sum[wave][1] = max_t; }
     __syncthreads();
-    if (!idle) { u = s_start[0]; sub = s_start[1]; }
+    if (tid == 0) arrive();
+    max_t = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      if (w < wave) pre_t += w_sum[w][0];
+      total += w_sum[w][0];
+      max_t = max(max_t, w_sum[w][1]);
+    }
+    while (team > 1 && U * team > grid * NW) team /= 2;
+    by_team = U * team <= grid * NW && max_t <= kTeamRounds * team;
+    if (by_team) {
+      u = wg * (NW / team) + wave / team;
+      idle = wg * (NW / team) >= U;
+    } else {
+      team = NW;
+      quota = (int)((uint32_t)(total + grid - 1) / (uint32_t)grid);
+      x = wg * quota;
+      idle = x >= total;
+      if (pre_t <= x && x < pre_t + my_t) {  // exactly one thread, if there is one
+        int at = pre_t, v = u0;
+        for (;; ++v) {
+          const int t = items_of(s_len[v]);
+          if (x < at + t) break;
+          at += t;
+        }
+        s_start[0] = v;
+        s_start[1] = x - at;
+      }
+      __syncthreads();
+      if (!idle) { u = s_start[0]; sub = s_start[1]; }
+    }
   }
 
   const int wt = team == NW ? wave : wave & (team - 1);
@@ -466,15 +561,17 @@ __global__ __launch_bounds__(NT, 2) void ag_q8_decode_kernel(dec_args a) {
   auto segment = [&]() {
     u = __builtin_amdgcn_readfirstlane(u);
     const bool mine = u < U;
-    const int sl = mine ? __builtin_amdgcn_readfirstlane(s_len[u]) : 0;
+    int sl = 0;
+    if constexpr (kRegs) sl = __builtin_amdgcn_readlane(u < 64 ? sl_r[0] : sl_r[1], u & 63);
+    else if (mine) sl = __builtin_amdgcn_readfirstlane(s_len[u]);
     const int n = sl & 0x7fffffff, nb = n / kQ8Block, T = nb + 1;
     int t0 = 0, t1 = mine ? T : 0, n_rec = 1, my_rec = 0, rec0 = 0;
     if (by_piece) {
-      n_rec = pieces_of(T, piece);
+      n_rec = pieces_of(T);
       my_rec = sub;
       rec0 = wg - sub;
       t0 = sub * piece;
-      t1 = min(T, t0 + piece);
+      if (n_rec > 1) t1 = min(T, t0 + piece);
     } else if (!by_team) {
       t0 = sub;
       t1 = min(T, t0 + left);
@@ -496,9 +593,16 @@ __global__ __launch_bounds__(NT, 2) void ag_q8_decode_kernel(dec_args a) {
     const bool has_tail = mine && t1 == T && (nb - t0) % team == wt;
     if (i0 < ip || has_tail) {
       const int32_t *page = a.c.page + (size_t)u * a.c.max_blocks;
+      // in one trip: page numbers, query, new key, positions; in the next: the page, the angles
+      const int id = i0 < ip ? page[i0] : 0, id_next = i0 < ip ? page[min(i0 + team, ip - 1)] : 0;
+      const typename wave_t::raw_t q_raw = wv.fetch(a.q + ((size_t)u * G + min(wv.head, G - 1)) * D);
+      typename wave_t::raw_t k_raw;
+      if (has_tail) k_raw = wv.fetch(a.k_new + (size_t)u * D);
+      q8_rows rows = {0, 0, 0};
+      if (a.rope.table) rows = q8_rope_rows(a.rope, u / a.Hkv, a.err);
+      if (i0 < ip) wv.first_page(a.c, __builtin_amdgcn_readfirstlane(id), __builtin_amdgcn_readfirstlane(id_next));
       float *angles = nullptr;
       if (a.rope.table) {  // into LDS: the query and the new key turn by the same
-        const q8_rows rows = q8_rope_rows(a.rope, u / a.Hkv, a.err);
         angles = s_angles[wave];
         if (own_lane < D / 2) {
           const float *row = q8_angle_row(a.rope, rows, own_lane, D) + own_lane;
@@ -507,11 +611,11 @@ __global__ __launch_bounds__(NT, 2) void ag_q8_decode_kernel(dec_args a) {
         }
         __builtin_amdgcn_wave_barrier();
       }
-      wv.query(a.q + (size_t)u * G * D, angles);
+      wv.query(q_raw, angles);
       uint4 nk[wave_t::KC][2];
       if (has_tail) {
         q8_eight y[wave_t::KC][2];
-        wv.vector(y, a.k_new + (size_t)u * D, angles);
+        wv.vector(y, k_raw, angles);
 #pragma unroll
         for (int c = 0; c < wave_t::KC; ++c)
 #pragma unroll
@@ -541,16 +645,25 @@ __global__ __launch_bounds__(NT, 2) void ag_q8_decode_kernel(dec_args a) {
     if (mine)
       for (int e = e0; e < G * D / 2; e += team * 64) {
         const int gg = e / (D / 2), d = 2 * (e - gg * (D / 2));
-        float M = kQ8EmptyMax, L = 0.f, A0 = 0.f, A1 = 0.f;
+        float M = kQ8EmptyMax, L = 0.f, A0 = 0.f, A1 = 0.f, ms[NW], ls[NW], o0[NW], o1[NW];
         const int w0 = wave - wt;
-        for (int w = 0; w < team; ++w) M = fmaxf(M, s_state[w0 + w][gg * SF]);
-        for (int w = 0; w < team; ++w) {
-          const float *st = s_state[w0 + w] + gg * SF;
-          if (st[1] == 0.f) continue;  // (a wave without rows)
-          const float f = __builtin_amdgcn_exp2f(st[0] - M);
-          L = fmaf(f, st[1], L);
-          A0 = fmaf(f, st[4 + d], A0);
-          A1 = fmaf(f, st[5 + d], A1);
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+          const float *st = s_state[w0 + (w < team ? w : 0)] + gg * SF;
+          ms[w] = w < team ? st[0] : kQ8EmptyMax;
+          ls[w] = w < team ? st[1] : 0.f;
+          o0[w] = st[4 + d];
+          o1[w] = st[5 + d];
+        }
+#pragma unroll
+        for (int w = 0; w < NW; ++w) M = fmaxf(M, ms[w]);
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+          const float f = __builtin_amdgcn_exp2f(ms[w] - M);
+          const bool any = !(ls[w] == 0.f);  // (a wave without rows)
+          L = fmaf(f, ls[w], L);
+          A0 = any ? fmaf(f, o0[w], A0) : A0;
+          A1 = any ? fmaf(f, o1[w], A1) : A1;
         }
         if (n_rec == 1) {
           store_out(gg, d, A0, A1, L);
@@ -609,6 +722,7 @@ __global__ __launch_bounds__(NT, 2) void ag_q8_decode_kernel(dec_args a) {
   // ---- the last workgroup to arrive counts the appended rows ----
   __syncthreads();
   if (tid == 0) {
+    if (kRegs) arrive();
     int last = grid - 1, order = s_order;
     if (groups > 1) {
       const int mine = (grid - wg % kDecodeArriveGroups + kDecodeArriveGroups - 1) / kDecodeArriveGroups;
@@ -619,21 +733,31 @@ __global__ __launch_bounds__(NT, 2) void ag_q8_decode_kernel(dec_args a) {
   }
   __syncthreads();
   if (!s_last) return;
+  if constexpr (kRegs) {
+    if (wave == 0)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        if (sl_r[j] < 0 && (!a.new_flags || a.new_flags[64 * j + lane] != 0)) a.c.len[64 * j + lane] = (sl_r[j] & 0x7fffffff) + 1;
+  } else
   for (int v = tid; v < U; v += NT)
     if (s_len[v] < 0 && (!a.new_flags || a.new_flags[v] != 0)) a.c.len[v] = (s_len[v] & 0x7fffffff) + 1;
   if (tid <= kDecodeArriveGroups) a.arrived[kDecodeArriveStride * tid] = 0;
 }
 
+template <int D, int G, int NW>
+hipError_t launch_nw(ag_ctx *ctx, hipStream_t s, const dec_args &a) {
+  // one workgroup per CU (8 waves) or two (4 waves), and no more than the step can have pieces
+  const int64_t most = a.U + (int64_t)a.U * (a.c.max_blocks + 1) / NW;
+  const int grid = (int)std::min<int64_t>((8 / NW) * ctx->num_cu, most);
+  static std::atomic<bool> allowed[64];
+  const hipError_t e = ag_q8_allow_lds(ctx->device, allowed, &ag_q8_decode_kernel<D, G, NW>, (size_t)kDecodeMaxUnits * 4);
+  if (e != hipSuccess) return e;
+  AG_LAUNCH(ag_time_kernel(ctx, AG_K_Q8_DECODE), (ag_q8_decode_kernel<D, G, NW>), dim3(grid), dim3(64 * NW), NW == 8 ? 0 : (size_t)a.U * 4, s, a);
+  return hipGetLastError();
+}
 template <int D, int G>
 hipError_t launch(ag_ctx *ctx, hipStream_t s, const dec_args &a) {
-  // one workgroup per CU, and no more than the step can have pieces
-  const int64_t most = a.U + (int64_t)a.U * (a.c.max_blocks + 1) / NW;
-  const int grid = (int)std::min<int64_t>(ctx->num_cu, most);
-  static std::atomic<bool> allowed[64];
-  const hipError_t e = ag_q8_allow_lds(ctx->device, allowed, &ag_q8_decode_kernel<D, G>, (size_t)kDecodeMaxUnits * 4);
-  if (e != hipSuccess) return e;
-  AG_LAUNCH(ag_time_kernel(ctx, AG_K_Q8_DECODE), (ag_q8_decode_kernel<D, G>), dim3(grid), dim3(NT), (size_t)a.U * 4, s, a);
-  return hipGetLastError();
+  return a.U <= kFewUnits ? launch_nw<D, G, 8>(ctx, s, a) : launch_nw<D, G, 4>(ctx, s, a);
 }
 template <int D>
 hipError_t launch_g(int G, ag_ctx *ctx, hipStream_t s, const dec_args &a) {
@@ -648,7 +772,7 @@ hipError_t launch_g(int G, ag_ctx *ctx, hipStream_t s, const dec_args &a) {
 
 }  // namespace
 
-size_t ag_ws_q8_decode_floats(int num_cu, int G, int D) { return (size_t)2 * num_cu * G * (D + 2); }
+size_t ag_ws_q8_decode_floats(int num_cu, int G, int D) { return (size_t)4 * num_cu * G * (D + 2); }
 
 hipError_t ag_launch_q8_decode(ag_ctx *ctx, hipStream_t s, const void *q, const void *k_new, const void *v_new, const uint8_t *new_flags,
                                int B, int Hq, int Hkv, int D, const ag_rope_dev &rope, float scale, const ag_q8_dev &cache, void *out, float *rec) {

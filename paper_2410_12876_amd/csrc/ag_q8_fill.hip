@@ -14,8 +14,9 @@ namespace {
 
 struct fill_args {
   const uint16_t *k, *v;
-  const uint64_t *words;
-  const int32_t *blk_off;
+  const uint8_t *flags;    // nullptr: every token is kept
+  uint64_t *words;         // the flags' masks and prefix counts: left by a unit's first workgroup, or read (CHUNKS = 0)
+  int32_t *blk_off;
   ag_q8_dev c;
   ag_rope_dev rope;
   uint16_t *tiles;
@@ -26,33 +27,104 @@ struct fill_args {
   int Hkv, L, nw, n_blk;
 };
 
-template <int D, bool TILES>
+// Sum over the lanes before this one; total: the wave's sum.
+__device__ __forceinline__ int wave_prefix(int x, int &total) {
+  int y = x;
+  y += __builtin_amdgcn_update_dpp(0, y, 0x111, 0xf, 0xf, false);
+  y += __builtin_amdgcn_update_dpp(0, y, 0x112, 0xf, 0xf, false);
+  y += __builtin_amdgcn_update_dpp(0, y, 0x114, 0xf, 0xf, false);
+  y += __builtin_amdgcn_update_dpp(0, y, 0x118, 0xf, 0xf, false);
+  y += __builtin_amdgcn_update_dpp(0, y, 0x142, 0xa, 0xf, false);
+  y += __builtin_amdgcn_update_dpp(0, y, 0x143, 0xc, 0xf, false);
+  total = __builtin_amdgcn_readlane(y, 63);
+  return y - x;
+}
+// The flags of 16 tokens from t on as bits (those past L: 0).  A row of flags starts at any address.
+__device__ __forceinline__ uint32_t flag_bits(const uint8_t *f, int t, int L) {
+  uint32_t bits = 0;
+  if (t + 16 <= L) {
+    uint32_t w[4];
+    __builtin_memcpy(w, f + t, 16);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t on = (((w[i] & 0x7f7f7f7fu) + 0x7f7f7f7fu) | w[i]) & 0x80808080u;  // the top bit of every byte that is not 0
+      bits |= (on >> 7 & 1) << (4 * i) | (on >> 15 & 1) << (4 * i + 1) | (on >> 23 & 1) << (4 * i + 2) | (on >> 31) << (4 * i + 3);
+    }
+  } else {
+    for (int i = 0; i < L - t; ++i) bits |= (uint32_t)(f[t + i] != 0) << i;
+  }
+  return bits;
+}
+
+// CHUNKS: pieces of 16 flags that a thread reads (the workgroup: all of the unit's); 0: they are taken from words and blk_off.
+template <int D, bool TILES, int CHUNKS>
 __global__ __launch_bounds__(256) void ag_q8_fill_kernel(fill_args a) {
   constexpr int KC = D / 64, VF = D / 64;  // K: chunks of 64 columns; V: pieces of 16 columns per wave
   constexpr int RS = D + 8;                // values per row of V in LDS (rows 4 apart start 16 banks apart)
   __shared__ __attribute__((aligned(16))) uint16_t s_v[kQ8Block * RS];
   __shared__ int32_t s_tok[kQ8Block], s_stop, s_order;
   __shared__ uint32_t s_top[2], s_least[2], s_odd;  // largest magnitudes of K, V; (TILES) those of their smallest rows; not finite
+  __shared__ int32_t s_sum[4];
   const int u = blockIdx.y, wg = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int most = a.c.max_blocks * kQ8Block + kQ8Block - 1;
   const int len0 = max(0, min(a.c.len[u], most));
-  const int held = len0 & (kQ8Block - 1), b0 = len0 / kQ8Block;
-  const int32_t *off = a.blk_off ? a.blk_off + (size_t)u * (a.nw + 1) : nullptr;
-  const int kept = off ? off[a.nw] : a.L;
-  const int32_t *page = a.c.page + (size_t)u * a.c.max_blocks;
-  // ---- rows that there is room for: up to the one that would fill the first block without a page ----
+  // ---- the kept tokens: this thread's flags and how many of the unit's lie before them ----
+  uint32_t bits[CHUNKS ? CHUNKS : 1];
+  int before = 0, mine = 0;
+  if constexpr (CHUNKS > 0) {
+    const int t = tid * 16 * CHUNKS;
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+      const int left = a.L - (t + 16 * i);
+      bits[i] = a.flags ? (left > 0 ? flag_bits(a.flags + (size_t)u * a.L, t + 16 * i, a.L) : 0u) : (left >= 16 ? 0xffffu : (1u << max(left, 0)) - 1u);
+      mine += __popc(bits[i]);
+    }
+  }
   if (tid == 0) s_stop = 0x7fffffff;
-  __syncthreads();
-  const int want = (held + kept) / kQ8Block;  // blocks to be filled
-  for (int j = tid; j < want; j += 256)
-    if (b0 + j >= a.c.max_blocks || (unsigned)page[min(b0 + j, a.c.max_blocks - 1)] >= (unsigned)a.c.n_pages) {
-      atomicMin(&s_stop, j);
+  const int held = len0 & (kQ8Block - 1), b0 = len0 / kQ8Block;
+  const int32_t *page = a.c.page + (size_t)u * a.c.max_blocks;
+  // ---- blocks of this call that may be filled and have no page: the first one ----
+  int stop = 0x7fffffff;
+  for (int j = tid; j < (held + a.L) / kQ8Block; j += 256)
+    if (b0 + j >= a.c.max_blocks || (uint32_t)page[min(b0 + j, a.c.max_blocks - 1)] >= (uint32_t)a.c.n_pages) {
+      stop = j;
       break;
     }
+  int kept;
+  const int32_t *off = nullptr;
+  if constexpr (CHUNKS > 0) {
+    int sum;
+    before = wave_prefix(mine, sum);
+    if (lane == 0) s_sum[wave] = sum;
+    __syncthreads();
+    kept = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      if (w < wave) before += s_sum[w];
+      kept += s_sum[w];
+    }
+    if (wg == 0 && a.words) {
+      int r = before;
+#pragma unroll
+      for (int i = 0; i < CHUNKS; ++i) {
+        const int t = tid * 16 * CHUNKS + 16 * i;
+        if (t < a.nw * 64) reinterpret_cast<uint16_t *>(a.words + (size_t)u * a.nw)[t / 16] = (uint16_t)bits[i];
+        if (t % 64 == 0 && t < a.nw * 64) a.blk_off[(size_t)u * (a.nw + 1) + t / 64] = r;
+        r += __popc(bits[i]);
+      }
+      if (tid == 0) a.blk_off[(size_t)u * (a.nw + 1) + a.nw] = kept;
+    }
+  } else {
+    if (a.flags) off = a.blk_off + (size_t)u * (a.nw + 1);
+    kept = off ? off[a.nw] : a.L;
+    __syncthreads();
+  }
+  if (stop < 0x7fffffff) atomicMin(&s_stop, stop);
   __syncthreads();
+  // rows that there is room for: up to the one that would fill the first block without a page
+  const int want = (held + kept) / kQ8Block;
   const int add = s_stop < want ? s_stop * kQ8Block + kQ8Block - 1 - held : kept;
   const int total = held + add, full = total / kQ8Block;
-  __syncthreads();
   if (tid == 0) {  // (len has been read)
     s_order = __hip_atomic_fetch_add(a.arrived + u, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     if (s_order == (int)gridDim.x - 1) {
@@ -86,10 +158,22 @@ __global__ __launch_bounds__(256) void ag_q8_fill_kernel(fill_args a) {
       }
     }
     __syncthreads();
-    if (!off) {
-      if (tid < kQ8Block && kk0 + tid >= 0 && kk0 + tid < add) s_tok[tid] = kk0 + tid;
+    const int hi = min(kk0 + kQ8Block, add);
+    if constexpr (CHUNKS > 0) {
+      int r = before;
+      if (r < hi && r + mine > kk0) {
+#pragma unroll
+        for (int i = 0; i < CHUNKS; ++i)
+#pragma unroll
+          for (int x = 0; x < 16; ++x)
+            if (bits[i] >> x & 1) {
+              if (r >= kk0 && r < hi) s_tok[r - kk0] = (tid * CHUNKS + i) * 16 + x;
+              ++r;
+            }
+      }
+    } else if (!off) {
+      if (tid < kQ8Block && kk0 + tid >= 0 && kk0 + tid < hi) s_tok[tid] = kk0 + tid;
     } else {
-      const int hi = min(kk0 + kQ8Block, add);
       for (int w = tid; w < a.nw; w += 256) {
         int r = off[w];
         if (r < hi && off[w + 1] > kk0) {
@@ -254,23 +338,36 @@ __global__ __launch_bounds__(256) void ag_q8_fill_kernel(fill_args a) {
 
 }  // namespace
 
-hipError_t ag_launch_q8_fill(ag_ctx *ctx, hipStream_t s, const void *k, const void *v, int B, int Hkv, int L, int D,
-                             const uint64_t *words, const int32_t *blk_off, const ag_rope_dev &rope, const ag_q8_dev &cache,
+// Up to here every workgroup counts the unit's flags itself (at most 64 a thread, in flight with the other first loads): 333 tokens of 8
+// heads 25 us with a scan launched before, XX without.  Beyond, a unit's flags are scanned once.
+int ag_q8_fill_flags() { return 4 * 16 * 256; }
+
+hipError_t ag_launch_q8_fill(ag_ctx *ctx, hipStream_t s, const void *k, const void *v, const uint8_t *flags, int B, int Hkv, int L, int D,
+                             uint64_t *words, int32_t *blk_off, const ag_rope_dev &rope, const ag_q8_dev &cache,
                              uint16_t *tiles, uint32_t *info, ag_q8_meta *meta) {
   fill_args a;
-  a.k = (const uint16_t *)k; a.v = (const uint16_t *)v;
+  a.k = (const uint16_t *)k; a.v = (const uint16_t *)v; a.flags = flags;
   a.words = words; a.blk_off = blk_off; a.c = cache; a.rope = rope;
   a.tiles = tiles; a.info = info; a.meta = meta;
   a.arrived = ctx->decode_tickets; a.err = ctx->d_err;
   a.Hkv = Hkv; a.L = L; a.nw = ag_nwords(L); a.n_blk = ag_q8_fill_blocks(L);
   const dim3 grid(a.n_blk, B * Hkv), block(256);
-#define AG_FILL(DD)                                                                                                              \
-  do {                                                                                                                           \
-    if (tiles) AG_LAUNCH(ag_time_kernel(ctx, AG_K_Q8_FILL), (ag_q8_fill_kernel<DD, true>), grid, block, 0, s, a);                \
-    else AG_LAUNCH(ag_time_kernel(ctx, AG_K_Q8_FILL), (ag_q8_fill_kernel<DD, false>), grid, block, 0, s, a);                     \
+  if (flags && L > ag_q8_fill_flags()) {
+    const hipError_t e = ag_launch_flag_scan(ctx, s, flags, B * Hkv, L, words, blk_off, nullptr);
+    if (e != hipSuccess) return e;
+  }
+#define AG_FILL(DD, TT, CC) AG_LAUNCH(ag_time_kernel(ctx, AG_K_Q8_FILL), (ag_q8_fill_kernel<DD, TT, CC>), grid, block, 0, s, a)
+#define AG_FILL_C(DD, TT)                       \
+  do {                                          \
+    if (L <= 4096) AG_FILL(DD, TT, 1);          \
+    else if (L <= 16384) AG_FILL(DD, TT, 4);    \
+    else AG_FILL(DD, TT, 0);                    \
   } while (0)
-  if (D == 128) AG_FILL(128);
-  else AG_FILL(64);
+  if (D == 128 && tiles) AG_FILL_C(128, true);
+  else if (D == 128) AG_FILL_C(128, false);
+  else if (tiles) AG_FILL_C(64, true);
+  else AG_FILL_C(64, false);
+#undef AG_FILL_C
 #undef AG_FILL
   return hipGetLastError();
 }
