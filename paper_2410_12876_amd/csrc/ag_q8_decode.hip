@@ -28,6 +28,9 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kFewUnits = 128;
 constexpr int kWholeRounds = 2;   // items of a wave up to which a unit is not cut: the meeting of the pieces costs as much as a round
 constexpr int kArriveSplit = 64;  // workgroups from which their arrivals are counted at several addresses
+// What a unit costs a workgroup beside its items, in items, where all units are cut into equal ranges: the start of a segment, the tail's two
+// bytes a value, the merge.  Without it the ranges that hold the most units end last.
+constexpr int kUnitCost = 7;
 constexpr int kTeamRounds = 6;    // items of a wave up to which units are given to teams of waves
 
 struct dec_args {
@@ -110,47 +113,18 @@ template <int D, int G> struct wave_q8 {
 #pragma unroll
     for (int f = 0; f < VF; ++f) o[f] = q8_f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  // This lane's 16 values of each 64 columns of a vector: as they lie in memory, then turned by the token's angles (in LDS:
-  // cosines, sines).
-  struct raw_t {
-    uint4 x[KC][2], p[KC == 2 ? 1 : 2];  // (KC = 1: the partners belong to another lane)
-  };
-  __device__ __forceinline__ raw_t fetch(const uint16_t *x) const {
-    raw_t r;
-#pragma unroll
-    for (int c = 0; c < KC; ++c)
-#pragma unroll
-      for (int s = 0; s < 2; ++s) r.x[c][s] = *reinterpret_cast<const uint4 *>(x + 64 * c + 16 * g + 8 * s);
-    if constexpr (KC == 1) {
-#pragma unroll
-      for (int s = 0; s < 2; ++s) r.p[s] = *reinterpret_cast<const uint4 *>(x + ((16 * g + 8 * s) ^ (D / 2)));
-    }
-    return r;
-  }
-  __device__ __forceinline__ void vector(q8_eight (&y)[KC][2], const raw_t &r, const float *angles) const {
+  // The query (turned, 32 bits, in LDS) in f16 (11 bits: a turned one in bf16 would shift the scores by 2^-9 of their size), its largest value in
+  // [2^14, 2^15)
+  __device__ __forceinline__ void query(const float *x) {
+    q8_eight y[KC][2];
+    float top = 0.f;
 #pragma unroll
     for (int c = 0; c < KC; ++c)
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        if (!angles) {
-          y[c][s] = q8_floats(r.x[c][s]);
-          continue;
-        }
-        uint4 p;
-        if constexpr (KC == 2) p = r.x[c ^ 1][s];
-        else p = r.p[s];
-        y[c][s] = q8_turn8<D>(
-            [&](int i) { return q8_angles{*reinterpret_cast<const float4 *>(angles + i), *reinterpret_cast<const float4 *>(angles + D / 2 + i)}; },
-            64 * c + 16 * g + 8 * s, r.x[c][s], p);
+        y[c][s] = eight_at(x, c, s);
+        top = fmaxf(top, y[c][s].top());
       }
-  }
-  // The query in f16 (11 bits: a turned one in bf16 would shift the scores by 2^-9 of their size), its largest value in [2^14, 2^15)
-  __device__ __forceinline__ void query(const raw_t &r, const float *angles) {
-    q8_eight y[KC][2];
-    vector(y, r, angles);
-    float top = 0.f;
-#pragma unroll
-    for (int c = 0; c < KC; ++c) top = fmaxf(top, fmaxf(y[c][0].top(), y[c][1].top()));
     top = kg_max(top);
     eq = max(kQ8TileMinExp, min(254, max(1, (int)(__float_as_uint(top) >> 23))) - 127 - kQ8TileTop);
     const float inv = q8_pow2(-eq);
@@ -158,6 +132,10 @@ template <int D, int G> struct wave_q8 {
     for (int c = 0; c < KC; ++c)
 #pragma unroll
       for (int s = 0; s < 2; ++s) qf[c][s] = y[c][s].f16(inv);
+  }
+  __device__ __forceinline__ q8_eight eight_at(const float *x, int c, int s) const {  // this lane's eight values of a vector
+    const q8_f32x4 *p = reinterpret_cast<const q8_f32x4 *>(x + 64 * c + 16 * g + 8 * s);
+    return q8_eight{p[0], p[1]};
   }
 
   // A new reference for the scores (their tile's exponent included): everything so far shrinks to it.
@@ -171,124 +149,146 @@ template <int D, int G> struct wave_q8 {
     }
   }
 
-  // Pages i0, i0 + step, ... < i1 of a unit: the first one is asked for before the query is there.
-  q8_u32x4 kr[KF], vr[VF];
-  float ks, vs;
-  int next;
-  bool ok;
-  __device__ __forceinline__ int id_of(const int32_t *page, int i) const { return __builtin_amdgcn_readfirstlane(page[i]); }
-  template <typename R> __device__ __forceinline__ void load(const uint8_t *pool, int p, R &r) const {  // every page is read once per step: non-temporal
-    const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)(pool + (size_t)p * (kQ8Block * D)), 0, kQ8Block * D, 0x00020000);
-#pragma unroll
-    for (int f = 0; f < (int)(sizeof(R) / sizeof(r[0])); ++f) r[f] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, lane * 16 + (f & 3) * 1024, f / 4 * 4096, 2);
+  // A wave's pages: lane x holds the number and the exponents of its page x (of at most 64 at a time); two pages are in flight.
+  int ids, ek_v, ev_v;
+  // (The same registers hold a tail instead: as long as the two were told apart the compiler kept room for both.)
+  q8_u32x4 buf[4 * KF];  // K of two pages, V of two pages; or a tail's K, V
+  uint32_t nv[VF / 2];   // this lane's values of the new token, two a register
+  __device__ __forceinline__ void numbers(const int32_t *page, int i0, int i1, int step) {
+    const int i = i0 + lane * step;
+    ids = i < i1 ? page[i] : -1;
   }
-  __device__ __forceinline__ void first_page(const ag_q8_dev &c, int id, int id_next) {
-    next = id_next;
-    ok = (uint32_t)id < (uint32_t)c.n_pages;
-    if (!ok) id = 0;
-    load(c.k, id, kr);
-    load(c.v, id, vr);
-    ks = c.k_scale[id]; vs = c.v_scale[id];
+  __device__ __forceinline__ void exponents(const ag_q8_dev &c) {
+    const bool ok = (uint32_t)ids < (uint32_t)c.n_pages;  // (a number outside the pool: rows that are not there)
+    const int id = ok ? ids : 0;
+    ek_v = (int)(__float_as_uint(c.k_scale[id]) >> 23) - 127;
+    ev_v = (int)(__float_as_uint(c.v_scale[id]) >> 23) - 127;
+    ids = ok ? ids : -1;
   }
-  // The state is kept relative to m, the largest score plus its page's exponent ev of V: a page's weights are 2^(score + ev - m) in f16, its values
-  // the codes, and its part of the row sum is 2^-ev the sum of its weights.
-  __device__ __forceinline__ void pages(const ag_q8_dev &c, const int32_t *page, int i0, int i1, int step, float qscale) {
-    float ks_next = 1.f, vs_next = 1.f;
-    bool fresh = true;
-    for (int i = i0; i < i1; i += step) {
-      const bool more = i + step < i1, now = ok;
-      int id = next;
-      if (more) {
-        ok = (uint32_t)id < (uint32_t)c.n_pages;
-        if (!ok) id = 0;
-        next = i + 2 * step < i1 ? id_of(page, i + 2 * step) : 0;
-        ks_next = c.k_scale[id]; vs_next = c.v_scale[id];
-      }
-      q8_f32x4 s[4];
+  template <int AT> __device__ __forceinline__ void load(const uint8_t *pool, int x) {  // every page is read once per step: non-temporal
+    const int id = max(0, __builtin_amdgcn_readlane(ids, x));
+    const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)(pool + (size_t)id * (kQ8Block * D)), 0, kQ8Block * D, 0x00020000);
 #pragma unroll
-      for (int a = 0; a < 4; ++a) {
-        s[a] = q8_f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int f = 0; f < KF; ++f) buf[AT + f] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, lane * 16 + (f & 3) * 1024, f / 4 * 4096, 2);
+  }
+  __device__ __forceinline__ void first_pages(const ag_q8_dev &c, int n) {
+    load<0>(c.k, 0);
+    load<2 * KF>(c.v, 0);
+    if (n > 1) {
+      load<KF>(c.k, 1);
+      load<3 * KF>(c.v, 1);
+    }
+  }
+  // Page x of n, which is in buffer B; that buffer's next one is asked for.  The state is kept relative to m, the largest score plus its page's
+  // exponent ev of V: a page's weights are 2^(score + ev - m) in f16, its values the codes, its part of the row sum 2^-ev the sum of its weights.
+  template <int B> __device__ __forceinline__ void one_page(const ag_q8_dev &c, int x, int n, float qscale, bool &fresh) {
+    const bool more = x + 2 < n, now = __builtin_amdgcn_readlane(ids, x) >= 0;
+    q8_f32x4 s[4];
 #pragma unroll
-        for (int cc = 0; cc < KC; ++cc)
+    for (int a = 0; a < 4; ++a) {
+      s[a] = q8_f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
-            s[a] = __builtin_amdgcn_mfma_f32_16x16x32_f16(q8_widen16(kr[a * KC + cc][2 * h], kr[a * KC + cc][2 * h + 1], 1.f), qf[cc][h], s[a], 0, 0, 0);
-      }
-      if (more) load(c.k, id, kr);
-      if (now) {  // (a page number outside the pool: rows that are not there)
-        auto exponent = [](float x) { return (int)(__builtin_amdgcn_readfirstlane(__float_as_uint(x)) >> 23) - 127; };
-        const int e = exponent(vs), ev = max(kQ8TileMinExp, e);
-        const float f = fmaxf(ldexpf(qscale, eq + exponent(ks)), 1.17549435e-38f);
-        float sum;
-        uint32_t w[8];
-        auto largest = [&] {
-          float mx = s[0][0];
+      for (int cc = 0; cc < KC; ++cc)
 #pragma unroll
-          for (int x = 1; x < 16; ++x) mx = fmaxf(mx, s[x >> 2][x & 3]);
-          return fmaxf(m, fmaf(kg_max(mx), f, (float)ev));
-        };
-        auto weigh = [&] {
-          const float off = (float)ev - m;
-          sum = 0.f;
+        for (int h = 0; h < 2; ++h)
+          s[a] = __builtin_amdgcn_mfma_f32_16x16x32_f16(q8_widen16(buf[B * KF + a * KC + cc][2 * h], buf[B * KF + a * KC + cc][2 * h + 1], 1.f), qf[cc][h], s[a], 0, 0, 0);
+    }
+    if (more) load<B * KF>(c.k, x + 2);
+    if (now) {
+      const int e = __builtin_amdgcn_readlane(ev_v, x), ev = max(kQ8TileMinExp, e);
+      const float f = fmaxf(ldexpf(qscale, eq + __builtin_amdgcn_readlane(ek_v, x)), 1.17549435e-38f);
+      float sum;
+      uint32_t w[8];
+      auto largest = [&] {
+        float mx = s[0][0];
 #pragma unroll
-          for (int x = 0; x < 8; ++x) {
-            const q8_f32x2 p = {__builtin_amdgcn_exp2f(fmaf(s[x >> 1][2 * (x & 1)], f, off)), __builtin_amdgcn_exp2f(fmaf(s[x >> 1][2 * (x & 1) + 1], f, off))};
-            sum += p[0] + p[1];
-            w[x] = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, q8_f16x2));
-          }
-        };
-        if (fresh) raise(largest());
-        fresh = false;
+        for (int y = 1; y < 16; ++y) mx = fmaxf(mx, s[y >> 2][y & 3]);
+        return fmaxf(m, fmaf(kg_max(mx), f, (float)ev));
+      };
+      auto weigh = [&] {
+        const float off = (float)ev - m;
+        sum = 0.f;
+#pragma unroll
+        for (int y = 0; y < 8; ++y) {
+          const q8_f32x2 p = {__builtin_amdgcn_exp2f(fmaf(s[y >> 1][2 * (y & 1)], f, off)), __builtin_amdgcn_exp2f(fmaf(s[y >> 1][2 * (y & 1) + 1], f, off))};
+          sum += p[0] + p[1];
+          w[y] = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, q8_f16x2));
+        }
+      };
+      if (fresh) raise(largest());
+      fresh = false;
+      weigh();
+      // no maximum in the common case: only where weights pass 2^15 is the reference moved (for that head alone)
+      if (__any(!(sum <= 32768.f))) {
+        const float m_new = largest();
+        raise(kg_max(sum <= 32768.f ? 0.f : 1.f) > 0.f ? m_new : m);
         weigh();
-        // no maximum in the common case: only where weights pass 2^15 is the reference moved (for that head alone)
-        if (__any(!(sum <= 32768.f))) {
-          const float m_new = largest();
-          raise(kg_max(sum <= 32768.f ? 0.f : 1.f) > 0.f ? m_new : m);
-          weigh();
-        }
-        l += ldexpf(sum, -ev);
-        const float scale = q8_pow2(e - ev);
-#pragma unroll
-        for (int x = 0; x < 8; ++x) w[x] = second ? 0u : w[x];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const q8_f16x8 pb = __builtin_bit_cast(q8_f16x8, make_uint4(w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3]));
-#pragma unroll
-          for (int x = 0; x < VF; ++x)
-            o[x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(q8_widen16(vr[x][2 * h], vr[x][2 * h + 1], scale), pb, o[x], 0, 0, 0);
-        }
       }
-      if (more) load(c.v, id, vr);
-      ks = ks_next; vs = vs_next;
+      l += ldexpf(sum, -ev);
+      const float scale = q8_pow2(e - ev);
+#pragma unroll
+      for (int y = 0; y < 8; ++y) w[y] = second ? 0u : w[y];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const q8_f16x8 pb = __builtin_bit_cast(q8_f16x8, make_uint4(w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3]));
+#pragma unroll
+        for (int y = 0; y < VF; ++y)
+          o[y] = __builtin_amdgcn_mfma_f32_16x16x32_f16(q8_widen16(buf[(2 + B) * KF + y][2 * h], buf[(2 + B) * KF + y][2 * h + 1], scale), pb, o[y], 0, 0, 0);
+      }
+    }
+    if (more) load<(2 + B) * KF>(c.v, x + 2);
+  }
+  // Pages i0, i0 + step, ... < i1 of a unit; the numbers and exponents of the first 64 are there, and up to two pages are asked for.
+  __device__ __forceinline__ void pages(const ag_q8_dev &c, const int32_t *page, int i0, int i1, int step, float qscale) {
+    bool fresh = true;
+    for (;;) {
+      const int n = min(64, (i1 - i0 + step - 1) / step);
+      for (int x = 0; x < n; x += 2) {
+        one_page<0>(c, x, n, qscale, fresh);
+        if (x + 1 < n) one_page<1>(c, x + 1, n, qscale, fresh);
+      }
+      i0 += 64 * step;
+      if (i0 >= i1) break;
+      numbers(page, i0, i1, step);
+      exponents(c);
+      first_pages(c, min(64, (i1 - i0 + step - 1) / step));
     }
   }
 
-  // The tail's n rows and the new token as row n (nk: this lane's part of its turned key); `append`: the new row stays.  The rows are bf16
+  // The tail's n rows and the new token as row n (its turned key in LDS); `append`: the new row stays.  The rows are bf16
   // of any size, so these products are in bf16: the query and the weights as the sum of two numbers each (the weights' second one
   // in the columns P further, which are idle otherwise).
-  __device__ __forceinline__ void tail(const dec_args &a, int u, int n, int block, bool append, const uint4 (&nk)[KC][2]) {
-    uint16_t *kt = a.c.k_tail + (size_t)u * kQ8Block * D, *vt = a.c.v_tail + (size_t)u * kQ8Block * D;
-    const uint16_t *vn = a.v_new + (size_t)u * D;
+  __device__ __forceinline__ void fetch_tail(const dec_args &a, int u, int n) {
+    const uint16_t *kt = a.c.k_tail + (size_t)u * kQ8Block * D, *vt = a.c.v_tail + (size_t)u * kQ8Block * D;
     // rows that are not there are not read (addresses past the descriptor's end give zeros)
     auto rsrc_of = [](const uint16_t *p) { return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, kQ8Block * D * 2, 0x00020000); };
     auto load = [](__amdgpu_buffer_rsrc_t rsrc, int at, bool there) {
-      return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, there ? at : 1 << 24, 0, 0));
+      return __builtin_amdgcn_raw_buffer_load_b128(rsrc, there ? at : 1 << 24, 0, 0);
     };
     const __amdgpu_buffer_rsrc_t k_rsrc = rsrc_of(kt), v_rsrc = rsrc_of(vt);
-    uint4 kr[4][KC][2], vr[VF][2];
 #pragma unroll
     for (int x = 0; x < 4; ++x)
 #pragma unroll
       for (int c = 0; c < KC; ++c)
 #pragma unroll
-        for (int s = 0; s < 2; ++s) kr[x][c][s] = load(k_rsrc, ((x * KC + c) * 64 + lane) * 32 + 16 * s, 16 * x + col < n);
+        for (int s = 0; s < 2; ++s) buf[(x * KC + c) * 2 + s] = load(k_rsrc, ((x * KC + c) * 64 + lane) * 32 + 16 * s, 16 * x + col < n);
 #pragma unroll
     for (int f = 0; f < VF; ++f)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) vr[f][i] = load(v_rsrc, (f * 64 + lane) * 32 + 16 * i, 32 * i + 4 * g < n);
-    uint32_t nv[VF / 2];  // this lane's values of the new token, two a register
+      for (int i = 0; i < 2; ++i) buf[2 * KF + 2 * f + i] = load(v_rsrc, (f * 64 + lane) * 32 + 16 * i, 32 * i + 4 * g < n);
+    const uint16_t *vn = a.v_new + (size_t)u * D;
 #pragma unroll
     for (int f = 0; f < VF / 2; ++f) nv[f] = (uint32_t)vn[32 * f + col] | (uint32_t)vn[32 * f + 16 + col] << 16;
+  }
+  __device__ __forceinline__ void tail(const dec_args &a, int u, int n, int block, bool append, const float *new_key) {
+    uint16_t *kt = a.c.k_tail + (size_t)u * kQ8Block * D, *vt = a.c.v_tail + (size_t)u * kQ8Block * D;
+    auto kr = [&](int x, int c, int s) -> q8_u32x4 & { return buf[(x * KC + c) * 2 + s]; };
+    auto vr = [&](int f, int i) -> q8_u32x4 & { return buf[2 * KF + 2 * f + i]; };
+    q8_u32x4 nk[KC][2];
+#pragma unroll
+    for (int c = 0; c < KC; ++c)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) nk[c][s] = __builtin_bit_cast(q8_u32x4, eight_at(new_key, c, s).bf16());
     // the new row joins: row n = 16 (n / 16) + col for K, = 16 i + 4 g + n % 4 for V
 #pragma unroll
     for (int x = 0; x < 4; ++x)
@@ -296,14 +296,14 @@ template <int D, int G> struct wave_q8 {
 #pragma unroll
         for (int c = 0; c < KC; ++c)
 #pragma unroll
-          for (int s = 0; s < 2; ++s) kr[x][c][s] = nk[c][s];
+          for (int s = 0; s < 2; ++s) kr(x, c, s) = nk[c][s];
       }
     const bool fills = append && n == kQ8Block - 1;  // the block is full: it goes to its page; else the row joins the tail
     if (append && !fills && col == (n & 15)) {
 #pragma unroll
       for (int c = 0; c < KC; ++c)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) *reinterpret_cast<uint4 *>(kt + q8_k_at<D>(n, c, g) * 16 + 8 * h) = nk[c][h];
+        for (int h = 0; h < 2; ++h) *reinterpret_cast<q8_u32x4 *>(kt + q8_k_at<D>(n, c, g) * 16 + 8 * h) = nk[c][h];
     }
     q8_f32x4 s[4];
 #pragma unroll
@@ -319,7 +319,7 @@ template <int D, int G> struct wave_q8 {
         const q8_bf16x8 qh = __builtin_bit_cast(q8_bf16x8, hi), ql = __builtin_bit_cast(q8_bf16x8, q8_eight{y.a - z.a, y.b - z.b}.bf16());
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-          const q8_bf16x8 k = __builtin_bit_cast(q8_bf16x8, kr[x][c][h]);
+          const q8_bf16x8 k = __builtin_bit_cast(q8_bf16x8, kr(x, c, h));
           s[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, ql, s[x], 0, 0, 0);
           s[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qh, s[x], 0, 0, 0);
         }
@@ -329,32 +329,32 @@ template <int D, int G> struct wave_q8 {
 #pragma unroll
     for (int x = 0; x < 4; ++x)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int row = 16 * x + 4 * g + r;
-        s[x][r] *= f;
-        if (row > n) s[x][r] = -INFINITY;
+      for (int i = 0; i < 4; ++i) {
+        const int row = 16 * x + 4 * g + i;
+        s[x][i] *= f;
+        if (row > n) s[x][i] = -INFINITY;
         // the new token: alone its weight is 1 whatever its score is; a score that overflowed to -infinity counts as the least number
-        if (row == n) s[x][r] = n == 0 && block == 0 ? 0.f : (s[x][r] < kQ8EmptyMax ? kQ8EmptyMax : s[x][r]);
-        mx = fmaxf(mx, s[x][r]);
+        if (row == n) s[x][i] = n == 0 && block == 0 ? 0.f : (s[x][i] < kQ8EmptyMax ? kQ8EmptyMax : s[x][i]);
+        mx = fmaxf(mx, s[x][i]);
       }
-    auto narrow = [](const uint4 &x, const uint4 &y, float inv) {
-      return make_uint4(q8_narrow(x.x, x.y, inv), q8_narrow(x.z, x.w, inv), q8_narrow(y.x, y.y, inv), q8_narrow(y.z, y.w, inv));
+    auto narrow = [](const q8_u32x4 &x, const q8_u32x4 &y, float inv) {
+      return q8_u32x4{q8_narrow(x[0], x[1], inv), q8_narrow(x[2], x[3], inv), q8_narrow(y[0], y[1], inv), q8_narrow(y[2], y[3], inv)};
     };
-    auto top4 = [](uint32_t top, const uint4 &w) { return q8_top(q8_top(q8_top(q8_top(top, w.x), w.y), w.z), w.w); };
+    auto top4 = [](uint32_t top, const q8_u32x4 &w) { return q8_top(q8_top(q8_top(q8_top(top, w[0]), w[1]), w[2]), w[3]); };
     const int id = fills ? a.c.page[(size_t)u * a.c.max_blocks + block] : 0;
     if (fills) {
       uint32_t top = 0;
 #pragma unroll
       for (int x = 0; x < 4; ++x)
 #pragma unroll
-        for (int c = 0; c < KC; ++c) top = top4(top4(top, kr[x][c][0]), kr[x][c][1]);
+        for (int c = 0; c < KC; ++c) top = top4(top4(top, kr(x, c, 0)), kr(x, c, 1));
       const int e = q8_exponent(wave_max(top));
       const float inv = q8_pow2(-e);
-      uint4 *to = reinterpret_cast<uint4 *>(a.c.k + (size_t)id * kQ8Block * D) + lane;
+      q8_u32x4 *to = reinterpret_cast<q8_u32x4 *>(a.c.k + (size_t)id * kQ8Block * D) + lane;
 #pragma unroll
       for (int x = 0; x < 4; ++x)
 #pragma unroll
-        for (int c = 0; c < KC; ++c) to[(x * KC + c) * 64] = narrow(kr[x][c][0], kr[x][c][1], inv);
+        for (int c = 0; c < KC; ++c) to[(x * KC + c) * 64] = narrow(kr(x, c, 0), kr(x, c, 1), inv);
       if (lane == 0) a.c.k_scale[id] = q8_pow2(e);
     }
     raise(fmaxf(m, kg_max(mx)));
@@ -376,20 +376,18 @@ template <int D, int G> struct wave_q8 {
     uint32_t old[8], mine[8];  // halves of word y (rows 16 (y / 2) + 4 g + 2 (y % 2) + 0, 1) that are rows before n, and row n
 #pragma unroll
     for (int y = 0; y < 8; ++y) {
-      const int r = 16 * (y / 2) + 4 * g + 2 * (y & 1);
-      old[y] = (r < n ? 0xffffu : 0u) | (r + 1 < n ? 0xffff0000u : 0u);
-      mine[y] = (r == n ? 0xffffu : 0u) | (r + 1 == n ? 0xffff0000u : 0u);
+      const int row = 16 * (y / 2) + 4 * g + 2 * (y & 1);
+      old[y] = (row < n ? 0xffffu : 0u) | (row + 1 < n ? 0xffff0000u : 0u);
+      mine[y] = (row == n ? 0xffffu : 0u) | (row + 1 == n ? 0xffff0000u : 0u);
     }
 #pragma unroll
     for (int f = 0; f < VF; ++f) {
       const uint32_t two = __builtin_amdgcn_perm(nv[f / 2], nv[f / 2], f & 1 ? 0x07060706u : 0x05040504u);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        uint4 &v = vr[f][i];
-        v.x = (v.x & old[4 * i]) | (two & mine[4 * i]);
-        v.y = (v.y & old[4 * i + 1]) | (two & mine[4 * i + 1]);
-        v.z = (v.z & old[4 * i + 2]) | (two & mine[4 * i + 2]);
-        v.w = (v.w & old[4 * i + 3]) | (two & mine[4 * i + 3]);
+        q8_u32x4 &v = vr(f, i);
+#pragma unroll
+        for (int y = 0; y < 4; ++y) v[y] = (v[y] & old[4 * i + y]) | (two & mine[4 * i + y]);
         o[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(q8_bf16x8, v),
                                                        __builtin_bit_cast(q8_bf16x8, make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3])), o[f], 0, 0, 0);
       }
@@ -401,12 +399,12 @@ template <int D, int G> struct wave_q8 {
     if (fills) {
       uint32_t top = 0;
 #pragma unroll
-      for (int f = 0; f < VF; ++f) top = top4(top4(top, vr[f][0]), vr[f][1]);
+      for (int f = 0; f < VF; ++f) top = top4(top4(top, vr(f, 0)), vr(f, 1));
       const int e = q8_exponent(wave_max(top));
       const float inv = q8_pow2(-e);
-      uint4 *to = reinterpret_cast<uint4 *>(a.c.v + (size_t)id * kQ8Block * D) + lane;
+      q8_u32x4 *to = reinterpret_cast<q8_u32x4 *>(a.c.v + (size_t)id * kQ8Block * D) + lane;
 #pragma unroll
-      for (int f = 0; f < VF; ++f) to[f * 64] = narrow(vr[f][0], vr[f][1], inv);
+      for (int f = 0; f < VF; ++f) to[f * 64] = narrow(vr(f, 0), vr(f, 1), inv);
       if (lane == 0) a.c.v_scale[id] = q8_pow2(e);
     }
   }
@@ -435,7 +433,7 @@ __global__ __launch_bounds__(64 * NW, 2) void ag_q8_decode_kernel(dec_args a) {
   constexpr int SF = wave_t::SF;
   constexpr bool kRegs = NW == 8;  // the work list lives in registers
   __shared__ __attribute__((aligned(16))) float s_state[NW][G * SF];
-  __shared__ __attribute__((aligned(16))) float s_angles[NW][D];
+  __shared__ __attribute__((aligned(16))) float s_turned[kRegs ? 1 : NW][(G + 1) * D];  // a team's queries and new key
   extern __shared__ int32_t s_len[];  // [U] rows held; top bit: another one fits
   __shared__ int32_t w_sum[NW][2], s_start[2], s_last, s_order;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -468,22 +466,38 @@ __global__ __launch_bounds__(64 * NW, 2) void ag_q8_decode_kernel(dec_args a) {
   };
   int sl_r[2] = {0, 0};                                                              // kRegs: this lane's units, lane and 64 + lane
   const int per = (U + NT - 1) / NT, u0 = min(U, tid * per), u1 = min(U, u0 + per);  // else this thread's
-  int total = 0, u = 0, sub = 0, team = NW, quota = 0, x = 0;
+  int total = 0, u = 0, sub = 0, team = NW, quota = 1, quota_2 = 1, x = 0;
   bool by_piece = false, by_team = false, idle;
+  // Equal ranges.  With two workgroups on a CU the one that came first is served first: 1024 units of up to 4096 rows, all ranges equal, the
+  // first halves of the launch ended after 84 us and the others after 94; so those get 8 % more.
+  const int half = NW == 8 || grid % 2 ? grid : grid / 2;
+  auto set_quotas = [&] {
+    quota = quota_2 = (int)((uint32_t)(total + grid - 1) / (uint32_t)grid);
+    if (half < grid) {
+      quota += quota / 25;
+      quota_2 = max(1, (int)((uint32_t)(max(0, total - half * quota) + half - 1) / (uint32_t)half));
+    }
+  };
+  auto range_of = [&](int at) {
+    return at < half * quota ? (int)((uint32_t)at / (uint32_t)quota) : half + (int)((uint32_t)(at - half * quota) / (uint32_t)quota_2);
+  };
+  auto range_at = [&](int r) { return r <= half ? r * quota : half * quota + (r - half) * quota_2; };
   if constexpr (kRegs) {  // (at most kFewUnits units: every wave by itself, without LDS and barriers)
-    int t[2] = {0, 0}, pre_t[2], pre_p[2] = {0, 0}, p[2] = {0, 0}, pieces = 0, sum;
+    int t[2] = {0, 0}, cost[2], pre_t[2], pre_p[2] = {0, 0}, p[2] = {0, 0}, pieces = 0, items = 0, sum;
 #pragma unroll
     for (int j = 0; j < 2; ++j)
       if (64 * j + lane < U) sl_r[j] = read_len(64 * j + lane);
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       if (64 * j + lane < U) t[j] = items_of(sl_r[j]);
-      pre_t[j] = total + wave_prefix(t[j], sum);
+      cost[j] = t[j] ? t[j] + kUnitCost : 0;
+      pre_t[j] = total + wave_prefix(cost[j], sum);
       total += sum;
     }
+    items = total - U * kUnitCost;
     // pieces of the fewest rounds of the waves for which every piece has a workgroup (sure for the second try)
     int rounds = 1;
-    if (total > NW * grid) rounds = (int)((uint32_t)(total + NW * grid - 1) / (uint32_t)(NW * grid));
+    if (items > NW * grid) rounds = (int)((uint32_t)(items + NW * grid - 1) / (uint32_t)(NW * grid));
     for (bool last = false;; last = true) {
       if (rounds > 1) set_rounds(rounds);
       pieces = 0;
@@ -494,16 +508,16 @@ __global__ __launch_bounds__(64 * NW, 2) void ag_q8_decode_kernel(dec_args a) {
         pieces += sum;
       }
       if (pieces <= grid || last || U >= grid) break;
-      rounds = max(rounds, (int)((uint32_t)(total + NW * (grid - U) - 1) / (uint32_t)(NW * (grid - U))));
+      rounds = max(rounds, (int)((uint32_t)(items + NW * (grid - U) - 1) / (uint32_t)(NW * (grid - U))));
     }
     // ... unless so many units are cut that the remainders of their last pieces weigh more than equal ranges cost
     by_piece = pieces <= grid && (rounds <= 2 || 4 * U <= grid);
-    if (!by_piece) quota = (int)((uint32_t)(total + grid - 1) / (uint32_t)grid);
-    x = by_piece ? wg : wg * quota;
+    if (!by_piece) set_quotas();
+    x = by_piece ? wg : range_at(wg);
     idle = x >= (by_piece ? pieces : total);
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const int from = by_piece ? pre_p[j] : pre_t[j], n = by_piece ? p[j] : t[j];
+      const int from = by_piece ? pre_p[j] : pre_t[j], n = by_piece ? p[j] : cost[j];
       const uint64_t hit = __ballot(from <= x && x < from + n);
       if (hit) {
         const int at = __builtin_ctzll(hit);
@@ -516,7 +530,7 @@ __global__ __launch_bounds__(64 * NW, 2) void ag_q8_decode_kernel(dec_args a) {
     for (int v = u0; v < u1; ++v) {
       const int n = read_len(v);
       s_len[v] = n;
-      my_t += items_of(n);
+      my_t += items_of(n) + kUnitCost;
       max_t = max(max_t, items_of(n));
     }
     int pre_t = wave_prefix(my_t, sum);
@@ -538,13 +552,13 @@ __global__ __launch_bounds__(64 * NW, 2) void ag_q8_decode_kernel(dec_args a) {
       idle = wg * (NW / team) >= U;
     } else {
       team = NW;
-      quota = (int)((uint32_t)(total + grid - 1) / (uint32_t)grid);
-      x = wg * quota;
+      set_quotas();
+      x = range_at(wg);
       idle = x >= total;
       if (pre_t <= x && x < pre_t + my_t) {  // exactly one thread, if there is one
         int at = pre_t, v = u0;
         for (;; ++v) {
-          const int t = items_of(s_len[v]);
+          const int t = items_of(s_len[v]) + kUnitCost;
           if (x < at + t) break;
           at += t;
         }
@@ -557,7 +571,7 @@ __global__ __launch_bounds__(64 * NW, 2) void ag_q8_decode_kernel(dec_args a) {
   }
 
   const int wt = team == NW ? wave : wave & (team - 1);
-  int left = idle || by_piece || by_team ? 0 : min(quota, total - x), at = x;
+  int left = idle || by_piece || by_team ? 0 : min(range_at(wg + 1), total) - x, at = x;
   auto segment = [&]() {
     u = __builtin_amdgcn_readfirstlane(u);
     const bool mine = u < U;
@@ -572,61 +586,76 @@ __global__ __launch_bounds__(64 * NW, 2) void ag_q8_decode_kernel(dec_args a) {
       rec0 = wg - sub;
       t0 = sub * piece;
       if (n_rec > 1) t1 = min(T, t0 + piece);
-    } else if (!by_team) {
-      t0 = sub;
-      t1 = min(T, t0 + left);
-      left -= t1 - t0;
-      const int first = at - t0;
-      at += t1 - t0;
+    } else if (!by_team) {  // item i of the unit lies at kUnitCost + i of its cost
+      const int c0 = sub, c1 = min(T + kUnitCost, c0 + left), first = at - c0;
+      left -= c1 - c0;
+      at += c1 - c0;
+      t0 = max(0, c0 - kUnitCost);
+      t1 = max(0, c1 - kUnitCost);
       if (t0 > 0 || t1 < T) {
-        const int g0 = first / quota, g1 = (first + T - 1) / quota;
+        const int g0 = range_of(first + kUnitCost), g1 = range_of(first + kUnitCost + T - 1);
         n_rec = g1 - g0 + 1;
         my_rec = wg - g0;
         rec0 = g0;
       }
     }
+    if (!by_team && t0 == t1) {  // (the range ends before the unit's first item)
+      ++u;
+      sub = 0;
+      return;
+    }
     wave_t wv;
     int own_lane = lane;  // (unknown to the compiler, which would compute all addresses ahead of the loop and keep them in memory)
     asm volatile("" : "+v"(own_lane));
     wv.init(own_lane);
-    const int i0 = t0 + wt, ip = min(t1, nb);
-    const bool has_tail = mine && t1 == T && (nb - t0) % team == wt;
-    if (i0 < ip || has_tail) {
-      const int32_t *page = a.c.page + (size_t)u * a.c.max_blocks;
-      // in one trip: page numbers, query, new key, positions; in the next: the page, the angles
-      const int id = i0 < ip ? page[i0] : 0, id_next = i0 < ip ? page[min(i0 + team, ip - 1)] : 0;
-      const typename wave_t::raw_t q_raw = wv.fetch(a.q + ((size_t)u * G + min(wv.head, G - 1)) * D);
-      typename wave_t::raw_t k_raw;
-      if (has_tail) k_raw = wv.fetch(a.k_new + (size_t)u * D);
-      q8_rows rows = {0, 0, 0};
-      if (a.rope.table) rows = q8_rope_rows(a.rope, u / a.Hkv, a.err);
-      if (i0 < ip) wv.first_page(a.c, __builtin_amdgcn_readfirstlane(id), __builtin_amdgcn_readfirstlane(id_next));
-      float *angles = nullptr;
-      if (a.rope.table) {  // into LDS: the query and the new key turn by the same
-        angles = s_angles[wave];
-        if (own_lane < D / 2) {
-          const float *row = q8_angle_row(a.rope, rows, own_lane, D) + own_lane;
-          angles[own_lane] = row[0];
-          angles[D / 2 + own_lane] = row[D / 2];
+    // item 0 is the tail, item i page i - 1
+    const bool has_tail = mine && t0 == 0 && wt == 0;
+    const int i0 = t0 + wt - 1 + (t0 + wt == 0 ? team : 0), ip = t1 - 1;
+    const int32_t *page = a.c.page + (size_t)u * a.c.max_blocks;
+    if (i0 < ip) wv.numbers(page, i0, ip, team);
+    int flag = 1;
+    if (has_tail) {
+      if (a.new_flags) flag = a.new_flags[u];
+      wv.fetch_tail(a, u, n & (kQ8Block - 1));
+    }
+    // the group's queries and the new key, turned, into LDS: a pair of values a thread
+    float *turned = s_turned[kRegs ? 0 : wave - wt];
+    if (mine && t0 < t1) {
+      const int n_vec = t0 == 0 ? G + 1 : G;
+      for (int e = own_lane + wt * 64; e < n_vec * (D / 2); e += team * 64) {
+        const int vec = e / (D / 2), i = e % (D / 2);
+        const uint16_t *x = vec < G ? a.q + ((size_t)u * G + vec) * D : a.k_new + (size_t)u * D;
+        const float lo = q8_lo(x[i]), hi = q8_lo(x[D / 2 + i]);
+        float c = 1.f, sn = 0.f;
+        if (a.rope.table) {
+          const int axis = i < a.rope.end0 ? 0 : (i < a.rope.end1 ? 1 : 2);
+          const float *row = a.rope.table + (size_t)q8_rope_row(a.rope, axis, u / a.Hkv, a.err) * D + i;
+          c = row[0];
+          sn = row[D / 2];
         }
-        __builtin_amdgcn_wave_barrier();
+        turned[vec * D + i] = a.rope.table ? q8_turn(lo, hi, c, sn, true) : lo;
+        turned[vec * D + D / 2 + i] = a.rope.table ? q8_turn(hi, lo, c, sn, false) : hi;
       }
-      wv.query(q_raw, angles);
-      uint4 nk[wave_t::KC][2];
+    }
+    if (i0 < ip) {
+      wv.exponents(a.c);
+    }
+    // (The pages are asked for behind this barrier: ahead of it they would stand in the way of the small loads that it waits for.  8 steps of
+    // 32 units of up to 13000 rows 169 us with both ahead, 162 with one, 153 with none.)
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (i0 < ip || has_tail) {
+      const int two = (ip - i0 > team) + 1;
+      if (i0 < ip && !has_tail) wv.first_pages(a.c, two);
+      wv.query(turned + min(wv.head, G - 1) * D);
       if (has_tail) {
-        q8_eight y[wave_t::KC][2];
-        wv.vector(y, k_raw, angles);
-#pragma unroll
-        for (int c = 0; c < wave_t::KC; ++c)
-#pragma unroll
-          for (int h = 0; h < 2; ++h) nk[c][h] = y[c][h].bf16();
+        flag = __builtin_amdgcn_readfirstlane(flag);
+        if (flag != 0 && sl >= 0 && lane == 0) atomicOr(a.err, 1);
+        wv.tail(a, u, n & (kQ8Block - 1), nb, flag != 0 && sl < 0, turned + G * D);
+        if (i0 < ip) wv.first_pages(a.c, two);
       }
-      wv.pages(a.c, page, i0, ip, team, a.qscale);
-      if (has_tail) {
-        const bool flag = !a.new_flags || a.new_flags[u] != 0;
-        if (flag && sl >= 0 && lane == 0) atomicOr(a.err, 1);
-        wv.tail(a, u, n & (kQ8Block - 1), nb, flag && sl < 0, nk);
-      }
+      if (i0 < ip) wv.pages(a.c, page, i0, ip, team, a.qscale);
     }
     wv.leave(s_state[wave]);
     __syncthreads();
