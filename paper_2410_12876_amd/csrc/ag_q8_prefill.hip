@@ -5,10 +5,15 @@
 // the full blocks of the cache are read as they are.  So the keys of a unit are one sequence of tiles -- its pages, then those --
 // of which row j sees the first `bound_j` rows; an evicted token's own key and value, which are in none of them, are what its state starts from.
 //   * A workgroup of 4 waves owns 128 query rows of a unit (token by token, the group's heads of a token side by side) and every wave 32 of
-//     them, with a lane owning one column: S^T = K q^T, O^T = V^T p^T on v_mfma_f32_32x32x16_bf16, P passes from the first product's
+//     them, with a lane owning one column: S^T = K q^T, O^T = V^T p^T on v_mfma_f32_32x32x16_f16, P passes from the first product's
 //     accumulators into the second one's operand without leaving the lane.
-//   * A tile's 64 rows go through registers into LDS in the order of the fragments; 8-bit codes become f16 there (exactly,
-//     one instruction for two values), once for the 128 rows.  The next tile's loads are in flight meanwhile.
+//   * A tile's 64 rows lie in LDS in the order of the fragments, in two buffers.  A page goes there through registers, its codes made f16
+//     (exactly, one instruction for two values) once for the 128 rows; a tile of this call, in that order already, is loaded into LDS
+//     directly.  Either way the next tile's loads are in flight while a tile is worked on.
+//   * A fragment is read four products before its own, and the two halves' products take turns, so that no product waits for LDS or for the
+//     product before it: 765 us in place of 900 for 4096 tokens of 8 heads in 2 groups over 13000 rows, with the pages' numbers and scales
+//     looked up 64 tiles at a time (tile by tile they were waited for in every step).  Forming one half's weights between the other half's
+//     products, which the compiler can be made to do, gained nothing over this: the second workgroup of the CU fills those gaps already.
 //   * Both products are in f16, whose 11 bits keep scores and weights to 2^-12 of themselves (in bf16, 2^-9: an output row's error grew from 1.7e-3
 //     to 2.9e-3 of its size, and with scores of 7 times the usual spread a weight was off by a hundredth).  Its narrow range is why queries and
 //     tiles carry exponents; tiles of too different values are taken row by row on the vector ALU.
@@ -160,106 +165,142 @@ __global__ __launch_bounds__(256, 2) void ag_q8_prefill_kernel(pf_args a) {
 
   const int32_t *page = a.c.page + (size_t)u * a.c.max_blocks;
   const uint16_t *tiles = a.tiles + (size_t)u * a.n_blk * 2 * HALF;
-  uint4 st[2 * NP];
-  bool have = false;  // the tile asked for is there (a page number outside the pool counts as evicted rows)
-  q8_tile_info info = {0, 0, false};
-  float v_scale = 1.f;
-  // a thread's two pieces of a page's V: rows 16 i + 4 g + 0..3 and 16 i + 4 (g + 2) + 0..3, i < 4, of column 16 f + r
-  const int vf = (tid >> 5) & (D / 16 - 1), vg = (tid >> 4) & 1, v_piece = (vf * 4 + vg) * 16 + (tid & 15);
   auto rsrc_of = [](const void *p, int bytes) { return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, bytes, 0x00020000); };
   auto load = [](__amdgpu_buffer_rsrc_t r, int at, int more) { return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(r, at, more, 0)); };
-  auto request = [&](int t) {
-    if (t < meta.blocks) {
-      const int p = page[t];
-      have = (unsigned)p < (unsigned)a.c.n_pages;
-      const int ps = have ? p : 0;
-      auto exponent = [](float x) { return (int)(__builtin_amdgcn_readfirstlane(__float_as_uint(x)) >> 23) - 127; };
-      const int e = exponent(a.c.v_scale[ps]);
-      info = q8_tile_info{exponent(a.c.k_scale[ps]), max(kQ8TileMinExp, e), false};
-      v_scale = q8_pow2(e - info.ev);
-      const __amdgpu_buffer_rsrc_t pk = rsrc_of(a.c.k + (size_t)ps * HALF, HALF), pv = rsrc_of(a.c.v + (size_t)ps * HALF, HALF);
-#pragma unroll
-      for (int x = 0; x < KC; ++x) st[x] = load(pk, tid * 16, x * 4096);
-      st[KC] = load(pv, v_piece * 16, 0);
-      st[KC + 1] = load(pv, v_piece * 16, 512);
-    } else {
-      have = true;
-      info = q8_tile_of(__builtin_amdgcn_readfirstlane(a.info[(size_t)u * a.n_blk + t - meta.blocks]));
-      const __amdgpu_buffer_rsrc_t w = rsrc_of(tiles + (size_t)(t - meta.blocks) * 2 * HALF, 4 * HALF);
-#pragma unroll
-      for (int x = 0; x < NP; ++x) st[x] = load(w, tid * 16, x * 4096);
-    }
-  };
-  auto stage = [&](int t, int buf) {
-    uint16_t *ks = smem + buf * 2 * HALF, *vs = ks + HALF;
-    if (t < meta.blocks) {
-#pragma unroll
-      for (int x = 0; x < KC; ++x) {
-        const int n = tid + 256 * x, r = n & 15, g = (n >> 4) & 3, c = (n >> 6) % KC, ra = (n >> 6) / KC, tt = 16 * ra + r;
-        uint16_t *to = ks + (((tt >> 5) * KS + 4 * c + g) * 64 + (tt & 31)) * 8;
-        *reinterpret_cast<q8_f16x8 *>(to) = q8_widen16(st[x].x, st[x].y, 1.f);
-        *reinterpret_cast<q8_f16x8 *>(to + 32 * 8) = q8_widen16(st[x].z, st[x].w, 1.f);
-      }
-      if (D == 128 || tid < 128) {
-        const uint32_t lo[4] = {st[KC].x, st[KC].y, st[KC].z, st[KC].w}, hi[4] = {st[KC + 1].x, st[KC + 1].y, st[KC + 1].z, st[KC + 1].w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          *reinterpret_cast<q8_f16x8 *>(vs + (((vf >> 1) * 4 + i) * 64 + vg * 32 + (vf & 1) * 16 + (tid & 15)) * 8) = q8_widen16(lo[i], hi[i], v_scale);
-      }
-    } else {
-#pragma unroll
-      for (int x = 0; x < NP; ++x) reinterpret_cast<uint4 *>(ks)[tid + 256 * x] = st[x];
-    }
-  };
-
+  // Lane x knows tile w_first + x: its page (0: a tile of this call; -1: not there, or odd) and its exponents.  (Read tile by tile, the
+  // page's number and then its scales would be waited for in every step.)
+  int w_first = t0, w_id = -1, w_ek = 0, w_ev = 0;
   bool any_odd = false;
+  auto look_up = [&](int first) {
+    const int t = first + lane;
+    bool odd = false;
+    w_first = first;
+    w_id = -1;
+    w_ek = w_ev = 0;
+    if (t < min(t1, meta.blocks)) {
+      const int p = page[t], ps = (uint32_t)p < (uint32_t)a.c.n_pages ? p : 0;  // (a page number outside the pool counts as evicted rows)
+      w_id = ps == p ? p : -1;
+      w_ek = (int)(__float_as_uint(a.c.k_scale[ps]) >> 23) - 127;
+      w_ev = (int)(__float_as_uint(a.c.v_scale[ps]) >> 23) - 127;
+    } else if (t < t1) {
+      const q8_tile_info info = q8_tile_of(a.info[(size_t)u * a.n_blk + t - meta.blocks]);
+      odd = info.odd;
+      w_id = odd ? -1 : 0;
+      w_ek = info.ek;
+      w_ev = info.ev;
+    }
+    any_odd |= __any(odd) != 0;
+  };
+  auto here = [&] {  // (the thread's number, unknown to the compiler: or all addresses below would be kept in registers)
+    int x = tid;
+    asm volatile("" : "+v"(x));
+    return x;
+  };
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(size_t)(__attribute__((address_space(3))) uint16_t *)smem);
+  uint4 rk[KC] = {}, rv[2] = {};  // a thread's pieces of the next page's K and V
+  // Tile t: a page into registers, a tile of this call, which lies as LDS wants it, into LDS by itself
+  auto request = [&](int t, int buf) {
+    const int id = __builtin_amdgcn_readlane(w_id, t - w_first), x = here();
+    if (id < 0) return;
+    if (t < meta.blocks) {
+      const __amdgpu_buffer_rsrc_t pk = rsrc_of(a.c.k + (size_t)id * HALF, HALF), pv = rsrc_of(a.c.v + (size_t)id * HALF, HALF);
+#pragma unroll
+      for (int i = 0; i < KC; ++i) rk[i] = load(pk, x * 16, i * 4096);
+      // rows 16 i + 4 g + 0..3 and 16 i + 4 (g + 2) + 0..3, i < 4, of column 16 f + r: f = x / 32, g = x / 16 % 2, r = x % 16 for thread x
+      const int at = ((x >> 5) & (D / 16 - 1)) * 1024 + (x & 31) * 16;
+      rv[0] = load(pv, at, 0);
+      rv[1] = load(pv, at, 512);
+    } else {
+      const __amdgpu_buffer_rsrc_t w = rsrc_of(tiles + (size_t)(t - meta.blocks) * 2 * HALF, 4 * HALF);
+      const uint32_t base = buf * 4 * HALF + wave * 1024;
+#pragma unroll
+      for (int i = 0; i < NP; ++i)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                     :: "s"(lds0 + base + i * 4096), "v"(x * 16), "s"(w), "s"(i * 4096) : "m0", "memory");
+    }
+  };
+  auto stage = [&](int t, int buf) {  // a page from the registers into LDS, widened
+    if (t >= meta.blocks) return;
+    uint16_t *ks = smem + buf * 2 * HALF, *vs = ks + HALF;
+    const int tid = here();
+#pragma unroll
+    for (int x = 0; x < KC; ++x) {
+      const int n = tid + 256 * x, r = n & 15, g = (n >> 4) & 3, c = (n >> 6) % KC, ra = (n >> 6) / KC, tt = 16 * ra + r;
+      uint16_t *to = ks + (((tt >> 5) * KS + 4 * c + g) * 64 + (tt & 31)) * 8;
+      *reinterpret_cast<q8_f16x8 *>(to) = q8_widen16(rk[x].x, rk[x].y, 1.f);
+      *reinterpret_cast<q8_f16x8 *>(to + 32 * 8) = q8_widen16(rk[x].z, rk[x].w, 1.f);
+    }
+    if (D == 128 || tid < 128) {
+      const int e = __builtin_amdgcn_readlane(w_ev, t - w_first);
+      const float scale = q8_pow2(e - max(kQ8TileMinExp, e));
+      const uint32_t lo[4] = {rv[0].x, rv[0].y, rv[0].z, rv[0].w}, hi[4] = {rv[1].x, rv[1].y, rv[1].z, rv[1].w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<q8_f16x8 *>(vs + (((tid >> 6) * 4 + i) * 64 + ((tid >> 4) & 1) * 32 + ((tid >> 5) & 1) * 16 + (tid & 15)) * 8) =
+            q8_widen16(lo[i], hi[i], scale);
+    }
+  };
   if (t0 < t1) {
-    request(t0);
+    look_up(t0);
+    request(t0, 0);
     stage(t0, 0);
   }
   for (int t = t0; t < t1; ++t) {
     const int buf = (t - t0) & 1;
-    const bool now = have;
-    const q8_tile_info it = info;
+    const bool now = __builtin_amdgcn_readlane(w_id, t - w_first) >= 0;
+    const int ek = __builtin_amdgcn_readlane(w_ek, t - w_first), e_v = max(kQ8TileMinExp, __builtin_amdgcn_readlane(w_ev, t - w_first));
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (what went to LDS by itself: the compiler does not know of it)
     __syncthreads();
-    if (t + 1 < t1) request(t + 1);
-    const int first = (t - meta.blocks) * kQ8Block;  // the tile's first row among the bf16 rows
-    any_odd |= it.odd;
-    if (now && first < see_one && !it.odd) {
-      const uint16_t *ks = smem + buf * 2 * HALF, *vs = ks + HALF;
+    if (t + 1 < t1) {
+      if (t + 1 - w_first >= 64) look_up(t + 1);
+      request(t + 1, buf ^ 1);
+    }
+    const int first = (t - meta.blocks) * kQ8Block;  // the tile's first row among those of the tiles of this call
+    if (now && first < see_one) {
+      const uint16_t *ks = smem + buf * 2 * HALF + lane * 8, *vs = ks + HALF;
       q8_f32x16 s[2];
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
+      for (int x = 0; x < 2; ++x)
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[x][i] = 0.f;
 #pragma unroll
-        for (int kk = 0; kk < KS; ++kk)
-          s[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const q8_f16x8 *>(ks + ((x * KS + kk) * 64 + lane) * 8), qx[kk], s[x], 0, 0, 0);
+      for (int kk = 0; kk < KS; ++kk)
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+          s[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const q8_f16x8 *>(ks + (x * KS + kk) * 512), qx[kk], s[x], 0, 0, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);  // fragments ahead of the products
+#pragma unroll
+      for (int x = 0; x < 2 * KS; ++x) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if (x + 4 < 2 * KS) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
       }
       // s[x][i]: row 32 x + 8 (i / 4) + 4 h + i % 4 of the tile.  The state is kept relative to m, the largest score plus its tile's ev: a
       // tile's weights are 2^(score + ev - m), at most 2^15, its values v 2^-ev, and its part of the row sum is 2^-ev the sum of its weights.
-      const float f = fmaxf(ldexpf(a.qscale, eq + it.ek), 1.17549435e-38f), ev = (float)it.ev;
+      const float f = fmaxf(ldexpf(a.qscale, eq + ek), 1.17549435e-38f), ev = (float)e_v;
       if (t >= meta.blocks && first + kQ8Block > see_all) {
+        const int b = bound - first - 4 * h;
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
           for (int i = 0; i < 16; ++i)
-            if (first + 32 * x + 8 * (i / 4) + 4 * h + i % 4 >= bound) s[x][i] = -INFINITY;
+            if (32 * x + 8 * (i / 4) + i % 4 >= b) s[x][i] = -INFINITY;
       }
-      q8_f16x2 p[2][8];
+      uint32_t p[2][8];
       float sum;
       auto weigh = [&] {
         const float off = ev - m;
-        sum = 0.f;
+        float part[2] = {0.f, 0.f};
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
           for (int i = 0; i < 16; i += 2) {
             const q8_f32x2 w = {__builtin_amdgcn_exp2f(fmaf(s[x][i], f, off)), __builtin_amdgcn_exp2f(fmaf(s[x][i + 1], f, off))};
-            sum += w[0] + w[1];
-            p[x][i / 2] = __builtin_convertvector(w, q8_f16x2);
-            if (i % 8 == 6) __builtin_amdgcn_sched_barrier(0);  // (all 32 at once would not fit the registers)
+            part[0] += w[0];
+            part[1] += w[1];
+            p[x][i / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(w, q8_f16x2));
+            asm volatile("" : "+v"(p[x][i / 2]));  // (packed here: the compiler would carry all 32 weights to the second product)
           }
+        sum = part[0] + part[1];
       };
       weigh();
       if (__any(!(sum <= 32768.f))) {  // the reference is too far below (or nothing yet): a new one, and the weights again
@@ -278,15 +319,20 @@ __global__ __launch_bounds__(256, 2) void ag_q8_prefill_kernel(pf_args a) {
         m = m_new;
         weigh();
       }
-      l += ldexpf(sum, -it.ev);
+      l += ldexpf(sum, -e_v);
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
+      for (int i = 0; i < 4; ++i) {
+        const q8_f16x8 pb = __builtin_bit_cast(q8_f16x8, make_uint4(p[i >> 1][4 * (i & 1)], p[i >> 1][4 * (i & 1) + 1], p[i >> 1][4 * (i & 1) + 2], p[i >> 1][4 * (i & 1) + 3]));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const q8_f16x2 *w = &p[i >> 1][4 * (i & 1)];
-          const q8_f16x8 pb = {w[0][0], w[0][1], w[1][0], w[1][1], w[2][0], w[2][1], w[3][0], w[3][1]};
-          o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const q8_f16x8 *>(vs + ((dt * 4 + i) * 64 + lane) * 8), pb, o[dt], 0, 0, 0);
-        }
+        for (int dt = 0; dt < DT; ++dt)
+          o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const q8_f16x8 *>(vs + (dt * 4 + i) * 512), pb, o[dt], 0, 0, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x100, 4, 1);
+#pragma unroll
+      for (int x = 0; x < 4 * DT; ++x) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+        if (x + 4 < 4 * DT) __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
+      }
     }
     if (t + 1 < t1) stage(t + 1, buf ^ 1);
   }
