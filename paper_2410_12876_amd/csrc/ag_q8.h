@@ -91,6 +91,8 @@ typedef __attribute__((__vector_size__(2 * sizeof(float)))) float q8_f32x2;
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float q8_f32x4;
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float q8_f32x16;
 typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t q8_u32x4;
+typedef __attribute__((__vector_size__(2 * sizeof(int16_t)))) int16_t q8_s16x2;
+typedef __attribute__((__vector_size__(2 * sizeof(uint16_t)))) uint16_t q8_u16x2;
 
 // Two floats to bf16, round to nearest even, lo in the lower half.
 __device__ __forceinline__ uint32_t q8_pack2(float lo, float hi) {
@@ -124,6 +126,12 @@ __device__ __forceinline__ uint32_t q8_narrow(uint32_t a, uint32_t b, float inv)
   };
   int w = __builtin_amdgcn_cvt_pk_fp8_f32(f(q8_lo(a)), f(q8_hi(a)), 0, false);
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f(q8_lo(b)), f(q8_hi(b)), w, true);
+}
+// The same for values known to be finite, of which none passes 448 scale = 448 2^e.
+__device__ __forceinline__ uint32_t q8_narrow_finite(uint32_t a, uint32_t b, float scale) {
+  q8_s16x2 w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(q8_s16x2{}, __builtin_bit_cast(q8_bf16x2, a), scale, false);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(q8_bf16x2, b), scale, true);
+  return __builtin_bit_cast(uint32_t, w);
 }
 // The larger of m and the magnitudes (as bits) of the two bf16 of a word; infinities and NaN do not count.
 __device__ __forceinline__ uint32_t q8_top(uint32_t m, uint32_t w) {
@@ -196,14 +204,22 @@ struct q8_eight {
 __device__ __forceinline__ q8_eight q8_floats(const uint4 &x) {
   return q8_eight{{q8_lo(x.x), q8_hi(x.x), q8_lo(x.y), q8_hi(x.y)}, {q8_lo(x.z), q8_hi(x.z), q8_lo(x.w), q8_hi(x.w)}};
 }
+// Eight values x of a vector turned, whose partners are p; a: four cosines, their sines, the next four cosines, their sines; lower: they
+// are of the vector's first half.
+__device__ __forceinline__ q8_eight q8_turn8(const q8_f32x4 (&a)[4], bool lower, const uint4 &x, const uint4 &p) {
+  const q8_eight u = q8_floats(x), w = q8_floats(p);
+  q8_eight y;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    y.a[i] = q8_turn(u.a[i], w.a[i], a[0][i], a[1][i], lower);
+    y.b[i] = q8_turn(u.b[i], w.b[i], a[2][i], a[3][i], lower);
+  }
+  return y;
+}
 // Values d .. d + 7 (x) of a vector of D turned, whose partners are p; angles(i): those of pairs i .. i + 3.
 template <int D, typename A> __device__ __forceinline__ q8_eight q8_turn8(A &&angles, int d, const uint4 &x, const uint4 &p) {
-  const bool lower = d < D / 2;
   const q8_angles e = angles(d & (D / 2 - 1)), f = angles((d & (D / 2 - 1)) + 4);
-  const q8_eight u = q8_floats(x), w = q8_floats(p);
-  return q8_eight{{q8_turn(u.a[0], w.a[0], e.c.x, e.s.x, lower), q8_turn(u.a[1], w.a[1], e.c.y, e.s.y, lower),
-                   q8_turn(u.a[2], w.a[2], e.c.z, e.s.z, lower), q8_turn(u.a[3], w.a[3], e.c.w, e.s.w, lower)},
-                  {q8_turn(u.b[0], w.b[0], f.c.x, f.s.x, lower), q8_turn(u.b[1], w.b[1], f.c.y, f.s.y, lower),
-                   q8_turn(u.b[2], w.b[2], f.c.z, f.s.z, lower), q8_turn(u.b[3], w.b[3], f.c.w, f.s.w, lower)}};
+  const q8_f32x4 a[4] = {{e.c.x, e.c.y, e.c.z, e.c.w}, {e.s.x, e.s.y, e.s.z, e.s.w}, {f.c.x, f.c.y, f.c.z, f.c.w}, {f.s.x, f.s.y, f.s.z, f.s.w}};
+  return q8_turn8(a, d < D / 2, x, p);
 }
 #endif
