@@ -3,16 +3,20 @@
 //
 // A step reads every page it attends to once: large steps are bound by HBM, small ones by dependent round trips.  The kernel builds
 // its own work list from len[] and hands data between workgroups only where a unit is too long for one.
-//   * Work is counted in items of one unit: its pages, and one for the tail and the new token.  A wave takes every NW-th item of its
+//   * Work is counted in items of one unit: one for the tail and the new token, then its pages.  A wave takes every NW-th item of its
 //     workgroup's segment.
-//   * A page holds 64 rows in the order of the matrix operands, so its 16-byte pieces go from memory into registers and there, widened
-//     to bf16 (exact, two values an instruction), into S^T = K q^T and O^T = V^T p^T on v_mfma_f32_16x16x32_bf16: no LDS, no barrier.  The next
-//     page's K is requested as soon as this one's is used up, its V likewise, so 8 to 16 KiB per wave are always in flight.
-//   * The 16 columns of a product are the G query heads of the group, several times: columns x and x + P (P = 4 or 8) have the same
-//     scores and carry the same weight's parts, P = 4: three bf16 numbers whose sum it is (24 bits), P = 8: two (16 bits).  That the columns
-//     would be idle otherwise makes the parts free.
+//   * A page holds 64 rows in the order of the matrix operands, so its 16-byte pieces go from memory into registers and there, made
+//     f16 (exact, two values an instruction), into S^T = K q^T and O^T = V^T p^T on v_mfma_f32_16x16x32_f16: no LDS, no barrier.  A wave has
+//     two pages in flight, 16 to 32 KiB; a piece's registers are asked for again as soon as it is used up.
+//   * Queries are f16 times a power of two per row, weights are f16 relative to a reference that is moved only when their sum passes 2^15:
+//     11 bits of each, as the codes have 4.  (A weight in three bf16 parts in the columns that G < 16 leaves idle was as exact and slower:
+//     32 sequences of 32 heads 533 us a 4 steps, now 440.)
+//   * The workgroup turns its queries and the new key together, into LDS: a lane's own row by itself took 64 lines a load.  The barrier
+//     after it waits for LDS alone, and the pages are asked for behind it: ahead of it they held up the small loads.
 //   * The tail is a page in bf16; the new token's row is put into it in registers, so that it is one row more.  The wave that has it also
 //     stores that row, or, if it is the block's last, the whole block in 8 bits.
+//   * 32 sequences of 32 heads over 400 to 4096 rows: 109 us a step, 5.2 TB/s of pages; a chat of 8 heads and hundreds of rows: 10 us, of
+//     which the launch and about six dependent round trips are all.
 //   * Segments: if the whole step gives every workgroup at most one piece of a unit (a few rounds of its waves), those; if there are more
 //     units than workgroups and all are short, one, two or four waves a unit; else all items end to end, in equal ranges.
 #include <algorithm>
@@ -23,15 +27,20 @@
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-// Up to here 8 waves per workgroup and one workgroup per CU: a unit's items are spread over as many waves as the registers allow;
-// beyond, 4 waves and two workgroups per CU, so that one streams while the other starts or merges.
+// Up to here 8 waves per workgroup and one workgroup per CU: a unit's items are spread over as many waves as the registers allow, and the
+// work list is held in them; beyond, 4 waves and two workgroups per CU, so that one streams while the other starts or merges.  A step with 8
+// (4) waves: 8 units of 13000 rows 16.3 (25.1) us, 32 of 777 16.6 (17.9), 128 of 8000 37.2 (39.6).
 constexpr int kFewUnits = 128;
-constexpr int kWholeRounds = 2;   // items of a wave up to which a unit is not cut: the meeting of the pieces costs as much as a round
+// Items of a wave up to which a unit is not cut: the meeting of the pieces costs as much as a round (64 units of 2000 rows 16.5 us, with 4
+// 19.4).
+constexpr int kWholeRounds = 2;
 constexpr int kArriveSplit = 64;  // workgroups from which their arrivals are counted at several addresses
 // What a unit costs a workgroup beside its items, in items, where all units are cut into equal ranges: the start of a segment, the tail's two
-// bytes a value, the merge.  Without it the ranges that hold the most units end last.
-constexpr int kUnitCost = 7;
-constexpr int kTeamRounds = 6;    // items of a wave up to which units are given to teams of waves
+// bytes a value, the merge.  Without it the ranges that hold the most units end last (a step with 0, 7, 14, 28: 128 units of 8000 rows 41.5,
+// 37.5, 35.1, 37.1 us, 256 of 4096 48, 43, 41, 42.5).
+constexpr int kUnitCost = 14;
+// Items of a wave up to which units are given to teams of waves (1024 units of 300 rows 25.6 us, of 700 32.3; cut into ranges 36.4 and 40.8).
+constexpr int kTeamRounds = 6;
 
 struct dec_args {
   const uint16_t *q, *k_new, *v_new;

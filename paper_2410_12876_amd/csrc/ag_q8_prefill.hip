@@ -28,7 +28,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kRows = 128;     // query rows of a workgroup
-constexpr int kMinTiles = 4;   // tiles of a piece, at least
+constexpr int kMinTiles = 4;   // tiles of a piece, at least (37 tokens over 777 rows 44.3 us; with 2 43.8, with 6 46, with 8 49.4; over 8000 alike)
 constexpr int kMaxSplit = 32;
 
 struct pf_args {
@@ -427,10 +427,13 @@ __global__ __launch_bounds__(256) void ag_q8_prefill_merge_kernel(pf_args a) {
       make_uint2(q8_pack2(o.x * inv, o.y * inv), q8_pack2(o.z * inv, o.w * inv));
 }
 
-// Pieces an item may be cut into: so many that the launch fills the workgroups the chip holds at once, from what the cache can hold at most.
-int splits(int num_cu, int U, int n_qt, int max_tiles) {
+// Pieces an item may be cut into, from what the cache can hold at most: so many that the launch fills every CU once (D = 64: twice, of the
+// three workgroups that fit).  More pieces balance better, but every one turns the queries again and is added up: 200 tokens of 8 heads in
+// groups of 4 over 5000 rows 75 us, with two a CU 82; 1024 tokens of 32 heads 69 and 78; head dimension 64, 2 x 900 tokens of 8 heads 106 us
+// with one, 99.5 with two, 106.5 with three or four.
+int splits(int num_cu, int D, int U, int n_qt, int max_tiles) {
   const int64_t items = (int64_t)U * n_qt;
-  const int64_t want = (2 * num_cu + items - 1) / items;
+  const int64_t want = ((D == 128 ? 1 : 2) * num_cu + items - 1) / items;
   return (int)std::max<int64_t>(1, std::min<int64_t>({want, (int64_t)kMaxSplit, (int64_t)(max_tiles + kMinTiles - 1) / kMinTiles}));
 }
 
@@ -463,7 +466,7 @@ void ag_q8_prefill_plan(int num_cu, int U, int Hq, int Hkv, int L, int D, int ma
   w->info = ws.take<uint32_t>((size_t)U * ag_q8_fill_blocks(L));
   w->meta = ws.take<ag_q8_meta>(U);
   w->n_qt = (int)(((int64_t)L * (Hq / Hkv) + kRows - 1) / kRows);
-  w->n_split = splits(num_cu, U, w->n_qt, max_blocks + ag_q8_fill_blocks(L));
+  w->n_split = splits(num_cu, D, U, w->n_qt, max_blocks + ag_q8_fill_blocks(L));
   w->part = w->n_split > 1 ? ws.take<float>((size_t)U * w->n_qt * w->n_split * kRows * (D + 4)) : nullptr;
 }
 
