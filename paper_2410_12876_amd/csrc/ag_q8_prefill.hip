@@ -82,10 +82,13 @@ __global__ __launch_bounds__(256, 2) void ag_q8_prefill_kernel(pf_args a) {
   extern __shared__ __attribute__((aligned(1024))) uint16_t smem[];  // two tiles: K fragments, V fragments
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, h = lane >> 5;
-  // block -> (piece, query tile, unit): long query tiles first, units next to each other
+  // block -> (piece, query tile, unit): long query tiles first, units next to each other but each time one further: blocks 8 apart are
+  // one XCD's, and a long unit that stayed with its XCD held the launch up (4096 tokens of 8 heads over up to 13000 rows 800 us, so 700; 4 x
+  // 600 tokens of 8 heads 152 and 125; the first 4096 of 32 heads 182 and 166), whatever its tiles in that L2 saved.
   int id = blockIdx.x;
-  const int u = id % a.U;
+  int u = id % a.U;
   id /= a.U;
+  u = (u + id) % a.U;
   const int piece = id % a.n_split, qt = a.n_qt - 1 - id / a.n_split;
   const ag_q8_meta meta = a.meta[u];
   const pf_cut cut = cut_of(a, meta, u, qt, G);
@@ -428,9 +431,9 @@ __global__ __launch_bounds__(256) void ag_q8_prefill_merge_kernel(pf_args a) {
 }
 
 // Pieces an item may be cut into, from what the cache can hold at most: so many that the launch fills every CU once (D = 64: twice, of the
-// three workgroups that fit).  More pieces balance better, but every one turns the queries again and is added up: 200 tokens of 8 heads in
-// groups of 4 over 5000 rows 75 us, with two a CU 82; 1024 tokens of 32 heads 69 and 78; head dimension 64, 2 x 900 tokens of 8 heads 106 us
-// with one, 99.5 with two, 106.5 with three or four.
+// three workgroups that fit).  More pieces balance better, but every one turns the queries again and is added up: 37 tokens of 8 heads in
+// groups of 4 over 8000 rows 57 us, with two a CU 66.7, 200 over 5000 75.3 and 71.1, 1500 over 3000 137 and 149, 1024 tokens of 32 heads 68.5
+// and 78; head dimension 64, 2 x 900 tokens of 8 heads over 5000 rows 106 us with one, 98.6 with two, 97.6 with four.
 int splits(int num_cu, int D, int U, int n_qt, int max_tiles) {
   const int64_t items = (int64_t)U * n_qt;
   const int64_t want = ((D == 128 ? 1 : 2) * num_cu + items - 1) / items;
