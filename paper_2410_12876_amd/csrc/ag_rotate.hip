@@ -2,13 +2,14 @@
 //   pair i of a vector (values i and i + D/2), angle row p = pos[axis(i)][token]:  y_i = x_i cos - x_(i+D/2) sin,
 //   y_(i+D/2) = x_(i+D/2) cos + x_i sin; products and sum rounded one by one in 32 bits, then once to the type.
 // Bound by memory: 2 (Hq + Hkv) tokens D values in and out.  A thread owns 16 bytes of a vector and the 16 bytes of their partners
-// for several heads of one token, so that the angles (as many bytes as two bf16 vectors) are read once for all of those; the loads
-// of four heads are in flight together.
+// for several heads of one token, so that the angles (as many bytes as two bf16 vectors) are read once for all of those.
+// 4096 tokens x 64 heads of 128 in bf16: 26.4 to 27 us, 5.0 to 5.2 TB/s; 2 x 2900 tokens x 40 heads of 64 in fp32, three axes: 24.6 us.
 #include "ag_q8.h"
 
 namespace {
 
-constexpr int kHeadsAtOnce = 4;
+// Heads whose loads are in flight together (1, 2, 4, 8: 27.2, 26.9, 27.0, 26.6 us in bf16, 24.0, 24.6, 25.0, 27.2 in fp32 at the sizes above).
+constexpr int kHeadsAtOnce = 2;
 
 template <typename T> __device__ __forceinline__ void unpack(const uint4 &x, float *f) {
   const uint32_t w[4] = {x.x, x.y, x.z, x.w};
@@ -89,7 +90,7 @@ hipError_t ag_launch_rotate(ag_ctx *ctx, hipStream_t s, const void *q, const voi
                             int D, const ag_rope_dev &rope, void *q_out, void *k_out) {
   const int tokens = B * L, E = dt == AG_BF16 ? 8 : 4, H = Hq + Hkv;
   const int64_t wgs = ((int64_t)tokens * (D / 2 / E) + 255) / 256;
-  // heads of a thread: as many as leave every CU several workgroups, at most 16
+  // heads of a thread: as many as leave every CU 8 workgroups, at most 16 (with 1 a CU: 27.2 us for 26.4, fp32 25.4 for 24.1)
   int heads = 16;
   while (heads > 1 && wgs * ((H + heads - 1) / heads) < 8 * ctx->num_cu) heads /= 2;
   const dim3 grid((unsigned)wgs, (H + heads - 1) / heads);
