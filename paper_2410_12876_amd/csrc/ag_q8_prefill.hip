@@ -95,6 +95,77 @@ __global__ __launch_bounds__(256, 2) void ag_q8_prefill_kernel(pf_args a) {
   const int t0 = piece * cut.per, t1 = min(cut.tiles, t0 + cut.per);
   if (piece > 0 && t0 >= t1) return;
 
+  // ---- this lane's query row ----
+  const int rows = a.L * G, b = u / a.Hkv;
+  auto row_of = [&](int c) { return qt * kRows + wave * 32 + c; };
+  auto token_of = [&](int row) { return min(row / G, a.L - 1); };
+  auto q_of = [&](int row) { return (((size_t)b * a.Hq + (size_t)(u % a.Hkv) * G + row % G) * a.L + token_of(row)) * D; };
+  const int j = token_of(row_of(col));
+  const size_t k_at = ((size_t)u * a.L + j) * D;
+  bool kept;
+  const int rank = rank_of(a, u, j, meta.added, kept);
+  const int bound = meta.held + rank + (kept ? 1 : 0);  // visible rows of those tiles
+  // The query in f16 times 2^eq (11 bits; bf16 would lose up to 2^-9 of a turned value, and the scores as much of themselves)
+  q8_rows at = {0, 0, 0};
+  auto angles = [&](int i) { return q8_angles4(a.rope, at, i, D); };
+  if (a.rope.table) at = q8_rope_rows(a.rope, (int64_t)b * a.L + j, a.err);
+  auto vector = [&](q8_eight (&y)[KS], const uint16_t *x) {  // this lane's half of a row, turned
+    uint4 raw[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) raw[ks] = *reinterpret_cast<const uint4 *>(x + 16 * ks + 8 * h);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+      y[ks] = a.rope.table ? q8_turn8<D>(angles, 16 * ks + 8 * h, raw[ks], raw[ks ^ (KS / 2)]) : q8_floats(raw[ks]);
+  };
+  q8_f16x8 qx[KS];
+  int eq;
+  {
+    q8_eight y[KS];
+    vector(y, a.q + q_of(row_of(col)));
+    float top = 0.f;  // (infinities are none of a binade's; NaN is passed over)
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) top = fmaxf(top, y[ks].top());
+    top = fmaxf(top, other_half(top));
+    eq = max(kQ8TileMinExp, min(254, max(1, (int)(__float_as_uint(top) >> 23))) - 127 - kQ8TileTop);
+    const float inv = q8_pow2(-eq);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qx[ks] = y[ks].f16(inv);
+  }
+  float m = kQ8EmptyMax, l = 0.f;
+  const bool alone = piece == 0 && !kept;  // an evicted token sees itself
+  if (alone) {
+    q8_eight y[KS];
+    vector(y, a.k + k_at);
+    float s = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s = fmaf((float)qx[ks][i], y[ks].a[i], fmaf((float)qx[ks][4 + i], y[ks].b[i], s));
+    s = (s + other_half(s)) * ldexpf(a.qscale, eq);
+    // seeing nothing else its weight is 1 whatever its score is; a score that overflowed to -infinity counts as the least number
+    m = meta.blocks == 0 && bound == 0 ? 0.f : (s < kQ8EmptyMax ? kQ8EmptyMax : s);
+    l = h == 0 ? 1.f : 0.f;  // (summed over the halves at the end)
+  }
+  q8_f32x16 o[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      uint2 w = make_uint2(0, 0);
+      if (alone) w = *reinterpret_cast<const uint2 *>(a.v + k_at + 32 * dt + 8 * x + 4 * h);
+      o[dt][4 * x] = q8_lo(w.x); o[dt][4 * x + 1] = q8_hi(w.x);
+      o[dt][4 * x + 2] = q8_lo(w.y); o[dt][4 * x + 3] = q8_hi(w.y);
+    }
+  // rows that every row of the wave sees, and that one of them sees
+  int see_all = bound, see_one = bound;
+#pragma unroll
+  for (int x = 16; x > 0; x >>= 1) {
+    see_all = min(see_all, __shfl_xor(see_all, x, 64));
+    see_one = max(see_one, __shfl_xor(see_one, x, 64));
+  }
+  see_all = __builtin_amdgcn_readfirstlane(see_all);
+  see_one = __builtin_amdgcn_readfirstlane(see_one);
+
   const int32_t *page = a.c.page + (size_t)u * a.c.max_blocks;
   const uint16_t *tiles = a.tiles + (size_t)u * a.n_blk * 2 * HALF;
   auto rsrc_of = [](const void *p, int bytes) { return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, bytes, 0x00020000); };
@@ -172,83 +243,11 @@ __global__ __launch_bounds__(256, 2) void ag_q8_prefill_kernel(pf_args a) {
             q8_widen16(lo[i], hi[i], scale);
     }
   };
-  if (t0 < t1) {  // (the first tile is on its way while the query is turned)
+  if (t0 < t1) {
     look_up(t0);
     request(t0, 0);
+    stage(t0, 0);
   }
-
-  // ---- this lane's query row ----
-  const int rows = a.L * G, b = u / a.Hkv;
-  auto row_of = [&](int c) { return qt * kRows + wave * 32 + c; };
-  auto token_of = [&](int row) { return min(row / G, a.L - 1); };
-  auto q_of = [&](int row) { return (((size_t)b * a.Hq + (size_t)(u % a.Hkv) * G + row % G) * a.L + token_of(row)) * D; };
-  const int j = token_of(row_of(col));
-  const size_t k_at = ((size_t)u * a.L + j) * D;
-  bool kept;
-  const int rank = rank_of(a, u, j, meta.added, kept);
-  const int bound = meta.held + rank + (kept ? 1 : 0);  // visible rows of those tiles
-  // The query in f16 times 2^eq (11 bits; bf16 would lose up to 2^-9 of a turned value, and the scores as much of themselves)
-  q8_rows at = {0, 0, 0};
-  auto angles = [&](int i) { return q8_angles4(a.rope, at, i, D); };
-  if (a.rope.table) at = q8_rope_rows(a.rope, (int64_t)b * a.L + j, a.err);
-  auto vector = [&](q8_eight (&y)[KS], const uint16_t *x) {  // this lane's half of a row, turned
-    uint4 raw[KS];
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) raw[ks] = *reinterpret_cast<const uint4 *>(x + 16 * ks + 8 * h);
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
-      y[ks] = a.rope.table ? q8_turn8<D>(angles, 16 * ks + 8 * h, raw[ks], raw[ks ^ (KS / 2)]) : q8_floats(raw[ks]);
-  };
-  q8_f16x8 qx[KS];
-  int eq;
-  {
-    q8_eight y[KS];
-    vector(y, a.q + q_of(row_of(col)));
-    float top = 0.f;  // (infinities are none of a binade's; NaN is passed over)
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) top = fmaxf(top, y[ks].top());
-    top = fmaxf(top, other_half(top));
-    eq = max(kQ8TileMinExp, min(254, max(1, (int)(__float_as_uint(top) >> 23))) - 127 - kQ8TileTop);
-    const float inv = q8_pow2(-eq);
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qx[ks] = y[ks].f16(inv);
-  }
-  float m = kQ8EmptyMax, l = 0.f;
-  const bool alone = piece == 0 && !kept;  // an evicted token sees itself
-  if (alone) {
-    q8_eight y[KS];
-    vector(y, a.k + k_at);
-    float s = 0.f;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) s = fmaf((float)qx[ks][i], y[ks].a[i], fmaf((float)qx[ks][4 + i], y[ks].b[i], s));
-    s = (s + other_half(s)) * ldexpf(a.qscale, eq);
-    // seeing nothing else its weight is 1 whatever its score is; a score that overflowed to -infinity counts as the least number
-    m = meta.blocks == 0 && bound == 0 ? 0.f : (s < kQ8EmptyMax ? kQ8EmptyMax : s);
-    l = h == 0 ? 1.f : 0.f;  // (summed over the halves at the end)
-  }
-  q8_f32x16 o[DT];
-#pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      uint2 w = make_uint2(0, 0);
-      if (alone) w = *reinterpret_cast<const uint2 *>(a.v + k_at + 32 * dt + 8 * x + 4 * h);
-      o[dt][4 * x] = q8_lo(w.x); o[dt][4 * x + 1] = q8_hi(w.x);
-      o[dt][4 * x + 2] = q8_lo(w.y); o[dt][4 * x + 3] = q8_hi(w.y);
-    }
-  // rows that every row of the wave sees, and that one of them sees
-  int see_all = bound, see_one = bound;
-#pragma unroll
-  for (int x = 16; x > 0; x >>= 1) {
-    see_all = min(see_all, __shfl_xor(see_all, x, 64));
-    see_one = max(see_one, __shfl_xor(see_one, x, 64));
-  }
-  see_all = __builtin_amdgcn_readfirstlane(see_all);
-  see_one = __builtin_amdgcn_readfirstlane(see_one);
-
-  if (t0 < t1) stage(t0, 0);
   for (int t = t0; t < t1; ++t) {
     const int buf = (t - t0) & 1;
     const bool now = __builtin_amdgcn_readlane(w_id, t - w_first) >= 0;
