@@ -235,6 +235,7 @@ __global__ __launch_bounds__(4 * D, 4) void ag_q8_fill_kernel(fill_args a) {
     if (n > 1) tokens(1);
     barrier();
     request(0);
+    if (n > 2) barrier();  // (block 0's list has been read: the first turn of the loop writes block 2's over it)
     turn_by();
   }
 #pragma unroll 1
