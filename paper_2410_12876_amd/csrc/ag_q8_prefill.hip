@@ -133,19 +133,6 @@ __global__ __launch_bounds__(256, 2) void ag_q8_prefill_kernel(pf_args a) {
   }
   float m = kQ8EmptyMax, l = 0.f;
   const bool alone = piece == 0 && !kept;  // an evicted token sees itself
-  if (alone) {
-    q8_eight y[KS];
-    vector(y, a.k + k_at);
-    float s = 0.f;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) s = fmaf((float)qx[ks][i], y[ks].a[i], fmaf((float)qx[ks][4 + i], y[ks].b[i], s));
-    s = (s + other_half(s)) * ldexpf(a.qscale, eq);
-    // seeing nothing else its weight is 1 whatever its score is; a score that overflowed to -infinity counts as the least number
-    m = meta.blocks == 0 && bound == 0 ? 0.f : (s < kQ8EmptyMax ? kQ8EmptyMax : s);
-    l = h == 0 ? 1.f : 0.f;  // (summed over the halves at the end)
-  }
   q8_f32x16 o[DT];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
@@ -156,6 +143,31 @@ __global__ __launch_bounds__(256, 2) void ag_q8_prefill_kernel(pf_args a) {
       o[dt][4 * x] = q8_lo(w.x); o[dt][4 * x + 1] = q8_hi(w.x);
       o[dt][4 * x + 2] = q8_lo(w.y); o[dt][4 * x + 3] = q8_hi(w.y);
     }
+  if (alone) {
+    q8_eight y[KS];
+    vector(y, a.k + k_at);
+    float s = 0.f, top = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s = fmaf((float)qx[ks][i], y[ks].a[i], fmaf((float)qx[ks][4 + i], y[ks].b[i], s));
+    s = (s + other_half(s)) * ldexpf(a.qscale, eq);
+    // Its value has an exponent as a tile has one: the reference is the score plus that, or the tiles' weights would be as much too small
+    // for f16 as the values are small.  (Values that are not finite do not count: other columns are not theirs.)
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(o[dt][i]) < INFINITY ? fabsf(o[dt][i]) : 0.f);
+    top = fmaxf(top, other_half(top));
+    int e = max(kQ8TileMinExp, max(1, (int)(__float_as_uint(top) >> 23)) - 127 - kQ8TileTop);
+    // seeing nothing else its weight is 1 whatever its score is; a score that overflowed to -infinity counts as the least number
+    if (meta.blocks == 0 && bound == 0) s = 0.f, e = 0;
+    m = (s < kQ8EmptyMax ? kQ8EmptyMax : s) + (float)e;
+    const float scale = q8_pow2(-e);
+    l = h == 0 ? scale : 0.f;  // (summed over the halves at the end)
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) o[dt] *= scale;
+  }
   // rows that every row of the wave sees, and that one of them sees
   int see_all = bound, see_one = bound;
 #pragma unroll

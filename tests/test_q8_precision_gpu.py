@@ -1,0 +1,82 @@
+"""How exactly the attention over the paged 8-bit cache computes, output row by output row, where sizes are far from 1.
+
+The bar of a row is on RMS(error) / RMS(row).  The store's rounding to bf16 (8 significant bits) moves an element by at most 2^-9 of
+itself, so it gives at most 2^-9 of the row.  Before it: queries, the call's own keys and values, and the weights are rounded to f16, each to within
+2^-12 / sqrt 3 = 1.4e-4 RMS of itself; a score of queries and keys of unit size times `spread` is then off by 2e-4 spread, a weight relatively by
+as much and by its own 1.4e-4.  A row that one or two keys make up shows a single draw of that: with five times its RMS, 1.2e-3
+max(1, spread) holds everything.  (bf16 operands would be 8 times that, weights below f16's normal range more.)"""
+import pytest
+import torch
+
+import paper_2410_12876_amd as ag
+import q8_reference as R
+from gpu_util import DEV, ensure_built
+from test_q8_gpu import BF, ctx_of, flags_of, gen, on_device, rope_of, some
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    ensure_built()
+
+
+def bar(spread=1.0):
+    return 2.0 ** -9 + 1.2e-3 * max(1.0, spread)
+
+
+def row_errors(got, want):
+    """RMS(error) / RMS(row) of every row of [..., D]"""
+    got, want = got.double().cpu(), want.double()
+    return ((got - want).pow(2).mean(-1) / want.pow(2).mean(-1)).sqrt()
+
+
+def cache_of(B, H, D, lens, room, g, values=0):
+    """A reference cache whose values are N(0, 1) times 2^values"""
+    blocks = (max(lens) + room) // 64 + 1
+    c = R.Cache(B, H, D, B * H * blocks, blocks, g, lens)
+    c.scales[1] *= 2.0 ** values
+    c.tails[1] *= 2.0 ** values
+    return c
+
+
+def turn_error(ref, g, q, k, v, f, scale, axes=0):
+    """The largest row error of a turn, and the rows' errors"""
+    B, Hq, L, D = q.shape
+    args, rope = rope_of(g, D, B, L, axes) if axes else (None, None)
+    dev, ctx, out = on_device(ref), ctx_of(ref, L, Hq), torch.empty(q.shape, dtype=BF, device=DEV)
+    ag.ag_q8_prefill_attn(ctx, q.to(DEV), k.to(DEV), v.to(DEV), f.to(DEV), rope, scale, dev, out)
+    ctx.poll_error()
+    q64, k64 = (R.turned64(q.float(), *args), R.turned64(k.float(), *args)) if axes else (q, k)
+    e = row_errors(out, R.attend(ref, q64, k64, v, f != 0, scale))
+    print("turn", tuple(q.shape), "row errors: mean %.2e, worst %.2e" % (e.mean().item(), e.max().item()), flush=True)
+    return e
+
+
+# ------------------------------------------------------------------------------------- sizes of values, tokens that are evicted
+@pytest.mark.parametrize("values", [0, -6, -10, -20, 20])
+@pytest.mark.parametrize("D,lens,axes", [(128, [0, 700], 1), (64, [130, 64], 0)])
+def test_turns_over_values_of_any_size(D, lens, axes, values):
+    g, L = gen(values + 100 + D), 300
+    ref = cache_of(1, 2, D, lens, L, g, values)
+    q, k, v, f = some(g, 1, 4, L, D), some(g, 1, 2, L, D), some(g, 1, 2, L, D) * 2.0 ** values, flags_of(g, "runs", 1, 2, L)
+    assert turn_error(ref, g, q, k, v, f, D ** -0.5, axes).max() <= bar()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_turns_whose_evicted_tokens_see_mostly_themselves(D):
+    """Scores of a token with itself up to 11, those with others of unit size; its own value up to 2^-12 of theirs."""
+    g, L = gen(D + 5), 260
+    ref = cache_of(1, 2, D, [90, 400], L, g)
+    q, v, f = some(g, 1, 2, L, D), some(g, 1, 2, L, D), flags_of(g, "runs", 1, 2, L)
+    own = torch.rand(1, 2, L, 1, generator=g)
+    k = torch.where(f[..., None] != 0, some(g, 1, 2, L, D), (q * own).to(BF))
+    v = torch.where(f[..., None] != 0, v, v * 2.0 ** -torch.randint(0, 13, (1, 2, L, 1), generator=g)).to(BF)
+    assert turn_error(ref, g, q, k, v, f, D ** -0.5).max() <= bar()
+
+
+def test_a_turn_that_is_cut_into_pieces_over_small_values():
+    g, L, D = gen(8), 40, 128
+    ref = cache_of(1, 2, D, [2500, 1400], L, g, -9)
+    q, k, v, f = some(g, 1, 8, L, D), some(g, 1, 2, L, D), some(g, 1, 2, L, D) * 2.0 ** -9, flags_of(g, "rand", 1, 2, L)
+    assert turn_error(ref, g, q, k, v, f, D ** -0.5, 1).max() <= bar()
