@@ -100,6 +100,11 @@ __device__ __forceinline__ float kg_sum(float x) {
   const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
+// x as bf16 in the lower half of a word, what is left of it as bf16 in the upper one
+__device__ __forceinline__ float in_two(float x) {
+  const float first = q8_lo(q8_pack2(x, 0.f));
+  return __uint_as_float(q8_pack2(first, fabsf(first) < INFINITY ? x - first : 0.f));
+}
 // x of the lane N columns further (of 16, cyclic)
 template <int N> __device__ __forceinline__ float column(float x) {
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 + (16 - N), 0xf, 0xf, false));
@@ -264,7 +269,7 @@ template <int D, int G> struct wave_q8 {
     }
   }
 
-  // The tail's n rows and the new token as row n (its turned key in LDS); `append`: the new row stays.  The rows are bf16
+  // The tail's n rows and the new token as row n (its turned key in LDS, in_two); `append`: the new row stays.  The rows are bf16
   // of any size, so these products are in bf16: the query and the weights as the sum of two numbers each (the weights' second one
   // in the columns P further, which are idle otherwise).
   __device__ __forceinline__ void fetch_tail(const dec_args &a, int u, int n) {
@@ -289,15 +294,24 @@ template <int D, int G> struct wave_q8 {
 #pragma unroll
     for (int f = 0; f < VF / 2; ++f) nv[f] = (uint32_t)vn[32 * f + col] | (uint32_t)vn[32 * f + 16 + col] << 16;
   }
-  __device__ __forceinline__ void tail(const dec_args &a, int u, int n, int block, bool append, const float *new_key) {
+  __device__ __forceinline__ void tail(const dec_args &a, int u, int n, int block, bool append, const uint32_t *new_key) {
     uint16_t *kt = a.c.k_tail + (size_t)u * kQ8Block * D, *vt = a.c.v_tail + (size_t)u * kQ8Block * D;
     auto kr = [&](int x, int c, int s) -> q8_u32x4 & { return buf[(x * KC + c) * 2 + s]; };
     auto vr = [&](int f, int i) -> q8_u32x4 & { return buf[2 * KF + 2 * f + i]; };
-    q8_u32x4 nk[KC][2];
+    q8_u32x4 nk[KC][2], nl[KC][2];  // the new key as it is held, and (in its row's lanes) what that rounding left over: its score is not off by it
 #pragma unroll
     for (int c = 0; c < KC; ++c)
 #pragma unroll
-      for (int s = 0; s < 2; ++s) nk[c][s] = __builtin_bit_cast(q8_u32x4, eight_at(new_key, c, s).bf16());
+      for (int s = 0; s < 2; ++s) {
+        const q8_u32x4 *p = reinterpret_cast<const q8_u32x4 *>(new_key + 64 * c + 16 * g + 8 * s);
+        const q8_u32x4 x[2] = {p[0], p[1]};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t even = x[i / 2][2 * (i & 1)], odd = x[i / 2][2 * (i & 1) + 1];
+          nk[c][s][i] = __builtin_amdgcn_perm(odd, even, 0x05040100u);
+          nl[c][s][i] = col == (n & 15) ? __builtin_amdgcn_perm(odd, even, 0x07060302u) : 0u;
+        }
+      }
     // the new row joins: row n = 16 (n / 16) + col for K, = 16 i + 4 g + n % 4 for V
 #pragma unroll
     for (int x = 0; x < 4; ++x)
@@ -314,7 +328,7 @@ template <int D, int G> struct wave_q8 {
 #pragma unroll
         for (int h = 0; h < 2; ++h) *reinterpret_cast<q8_u32x4 *>(kt + q8_k_at<D>(n, c, g) * 16 + 8 * h) = nk[c][h];
     }
-    q8_f32x4 s[4];
+    q8_f32x4 s[4], s_new = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int x = 0; x < 4; ++x) s[x] = q8_f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -332,6 +346,7 @@ template <int D, int G> struct wave_q8 {
           s[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, ql, s[x], 0, 0, 0);
           s[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qh, s[x], 0, 0, 0);
         }
+        s_new = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(q8_bf16x8, nl[c][h]), qh, s_new, 0, 0, 0);
       }
     const float f = fmaxf(ldexpf(a.qscale, eq), 1.17549435e-38f);
     float mx = -INFINITY;
@@ -340,7 +355,7 @@ template <int D, int G> struct wave_q8 {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int row = 16 * x + 4 * g + i;
-        s[x][i] *= f;
+        s[x][i] = (x == n / 16 ? s[x][i] + s_new[i] : s[x][i]) * f;
         if (row > n) s[x][i] = -INFINITY;
         // the new token: alone its weight is 1 whatever its score is; a score that overflowed to -infinity counts as the least number
         if (row == n) s[x][i] = n == 0 && block == 0 ? 0.f : (s[x][i] < kQ8EmptyMax ? kQ8EmptyMax : s[x][i]);
@@ -642,8 +657,13 @@ __global__ __launch_bounds__(64 * NW, 2) void ag_q8_decode_kernel(dec_args a) {
           c = row[0];
           sn = row[D / 2];
         }
-        turned[vec * D + i] = a.rope.table ? q8_turn(lo, hi, c, sn, true) : lo;
-        turned[vec * D + D / 2 + i] = a.rope.table ? q8_turn(hi, lo, c, sn, false) : hi;
+        float y = a.rope.table ? q8_turn(lo, hi, c, sn, true) : lo, z = a.rope.table ? q8_turn(hi, lo, c, sn, false) : hi;
+        if (vec == G) {  // the new key: bf16, and what that leaves over (half a word each)
+          y = in_two(y);
+          z = in_two(z);
+        }
+        turned[vec * D + i] = y;
+        turned[vec * D + D / 2 + i] = z;
       }
     }
     if (i0 < ip) {
@@ -661,7 +681,7 @@ __global__ __launch_bounds__(64 * NW, 2) void ag_q8_decode_kernel(dec_args a) {
       if (has_tail) {
         flag = __builtin_amdgcn_readfirstlane(flag);
         if (flag != 0 && sl >= 0 && lane == 0) atomicOr(a.err, 1);
-        wv.tail(a, u, n & (kQ8Block - 1), nb, flag != 0 && sl < 0, turned + G * D);
+        wv.tail(a, u, n & (kQ8Block - 1), nb, flag != 0 && sl < 0, reinterpret_cast<const uint32_t *>(turned + G * D));
         if (i0 < ip) wv.first_pages(a.c, two);
       }
       if (i0 < ip) wv.pages(a.c, page, i0, ip, team, a.qscale);

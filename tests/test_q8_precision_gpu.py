@@ -80,3 +80,52 @@ def test_a_turn_that_is_cut_into_pieces_over_small_values():
     ref = cache_of(1, 2, D, [2500, 1400], L, g, -9)
     q, k, v, f = some(g, 1, 8, L, D), some(g, 1, 2, L, D), some(g, 1, 2, L, D) * 2.0 ** -9, flags_of(g, "rand", 1, 2, L)
     assert turn_error(ref, g, q, k, v, f, D ** -0.5, 1).max() <= bar()
+
+
+# ----------------------------------------------------------------------------------------------------------------- one new token
+def many_units(B, H, D, longest, g, values=0):
+    """A reference cache of units of 0 to `longest` rows (one of them the longest) on a few pages that they share; each unit's last block has
+    a page of its own."""
+    U = B * H
+    lens = torch.randint(0, longest + 1, (U,), generator=g).tolist()
+    lens[U // 2] = longest
+    page = torch.randint(U, U + 9, (U, longest // 64 + 1), generator=g).int()
+    for u in range(U):
+        page[u, lens[u] // 64] = u
+    c = R.Cache(B, H, D, U + 9, longest // 64 + 1, g, lens, page=page)
+    c.scales[1] *= 2.0 ** values
+    c.tails[1] *= 2.0 ** values
+    return c
+
+
+def step_error(ref, g, q, k, v, f, scale, axes=0):
+    """The row errors of a step"""
+    B, Hq, D = q.shape
+    args, rope = rope_of(g, D, B, 1, axes) if axes else (None, None)
+    dev, ctx, out = on_device(ref), ctx_of(ref, 1, Hq), torch.empty(q.shape, dtype=BF, device=DEV)
+    ag.ag_q8_decode_attn(ctx, q.to(DEV), k.to(DEV), v.to(DEV), f.to(DEV), rope, scale, dev, out)
+    ctx.poll_error()
+    q, k, v = q.unsqueeze(2), k.unsqueeze(2), v.unsqueeze(2)
+    q64, k64 = (R.turned64(q.float(), *args), R.turned64(k.float(), *args)) if axes else (q, k)
+    e = row_errors(out, R.attend(ref, q64, k64, v, torch.ones(v.shape[:3], dtype=torch.bool), scale)[:, :, 0])
+    print("step", tuple(q.shape), "row errors: mean %.2e, worst %.2e" % (e.mean().item(), e.max().item()), flush=True)
+    return e
+
+
+@pytest.mark.parametrize("B,H,G,D,longest", [(20, 8, 1, 128, 500), (20, 8, 1, 64, 500), (4, 4, 4, 128, 900), (70, 4, 2, 64, 300)])
+def test_steps_whose_new_token_has_half_of_the_weight_at_large_scores(B, H, G, D, longest):
+    """Scores of seven times the usual size; the new token's is about the logarithm of the others' sum, for one head of a group."""
+    g, spread = gen(B + D + longest), 7.0
+    scale = spread * D ** -0.5
+    ref = many_units(B, H, D, longest, g)
+    q, k, v = some(g, B, H * G, D), some(g, B, H, D), some(g, B, H, D)
+    args, _ = rope_of(gen(5), D, B, 1, 1)
+    q64 = R.turned64(q.unsqueeze(2).float(), *args)
+    for u in range(B * H):
+        b, h = divmod(u, H)
+        K, one = ref.rows(u, 0), q[b, h * G].double()
+        others = torch.logsumexp(K @ q64[b, h * G, 0] * scale, 0) if K.shape[0] else torch.tensor(0.0)
+        k[b, h] = (k[b, h].double() + one * (others / scale - one @ k[b, h].double()) / (one @ one)).to(BF)
+    assert step_error(ref, gen(5), q, k, v, torch.ones(B, H, dtype=torch.uint8), scale, 1).max() <= bar(spread)
+
+
