@@ -38,6 +38,9 @@ struct q8_tile_info {
 constexpr int kQ8TileTop = 14;      // a tile's largest number lies in [2^14, 2^15) ...
 constexpr int kQ8TileMinExp = -60;  // ... unless that took a smaller exponent than this (sums of 2^-ev stay in range)
 constexpr int kQ8TileSpan = 16;
+// Weights are f16 relative to a reference that lies this many bits below the largest one when it is set: those down to 2^-22 of it
+// keep their 11 bits, those down to 2^-33 some, and a long cache's many small ones are not lost.
+constexpr int kQ8TopBits = 8;
 
 // What ag_q8_fill_kernel leaves for the attention of the same call: the unit's cache as it stood before it.
 struct ag_q8_meta {
@@ -188,6 +191,11 @@ __device__ __forceinline__ float q8_turn(float x, float p, float c, float s, boo
 #pragma clang fp contract(off)
   const float a = x * c, b = p * s;
   return lower ? a - b : a + b;
+}
+// The two f16 of a word added to x.
+__device__ __forceinline__ float q8_add2(uint32_t w, float x) {
+  const q8_f16x2 one = {(_Float16)1.f, (_Float16)1.f};
+  return __builtin_amdgcn_fdot2(__builtin_bit_cast(q8_f16x2, w), one, x, false);
 }
 // Eight values of a vector in 32 bits.
 struct q8_eight {

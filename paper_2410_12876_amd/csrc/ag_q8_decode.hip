@@ -34,6 +34,7 @@ constexpr int kFewUnits = 128;
 // Items of a wave up to which a unit is not cut: the meeting of the pieces costs as much as a round (64 units of 2000 rows 16.5 us, with 4
 // 19.4).
 constexpr int kWholeRounds = 2;
+constexpr int kValueBits = 9;     // a page's values in f16 are below 1 (exact: a code has 4 bits, the least is 2^-9), as the tail's are of unit size
 constexpr int kArriveSplit = 64;  // workgroups from which their arrivals are counted at several addresses
 // What a unit costs a workgroup beside its items, in items, where all units are cut into equal ranges: the start of a segment, the tail's two
 // bytes a value, the merge.  Without it the ranges that hold the most units end last (a step with 0, 7, 14, 28: 128 units of 8000 rows 41.5,
@@ -194,7 +195,8 @@ template <int D, int G> struct wave_q8 {
     }
   }
   // Page x of n, which is in buffer B; that buffer's next one is asked for.  The state is kept relative to m, the largest score plus its page's
-  // exponent ev of V: a page's weights are 2^(score + ev - m) in f16, its values the codes, its part of the row sum 2^-ev the sum of its weights.
+  // exponent ev of V less kQ8TopBits: a page's weights are 2^(score + ev - m) in f16, its values the codes 2^-kValueBits, its part of the row
+  // sum 2^-ev the sum of its weights (as the product takes them: what rounding them changes cancels).
   template <int B> __device__ __forceinline__ void one_page(const ag_q8_dev &c, int x, int n, float qscale, bool &fresh) {
     const bool more = x + 2 < n, now = __builtin_amdgcn_readlane(ids, x) >= 0;
     q8_f32x4 s[4];
@@ -209,7 +211,7 @@ template <int D, int G> struct wave_q8 {
     }
     if (more) load<B * KF>(c.k, x + 2);
     if (now) {
-      const int e = __builtin_amdgcn_readlane(ev_v, x), ev = max(kQ8TileMinExp, e);
+      const int e = __builtin_amdgcn_readlane(ev_v, x), ev = max(kQ8TileMinExp, e + kValueBits);
       const float f = fmaxf(ldexpf(qscale, eq + __builtin_amdgcn_readlane(ek_v, x)), 1.17549435e-38f);
       float sum;
       uint32_t w[8];
@@ -217,17 +219,18 @@ template <int D, int G> struct wave_q8 {
         float mx = s[0][0];
 #pragma unroll
         for (int y = 1; y < 16; ++y) mx = fmaxf(mx, s[y >> 2][y & 3]);
-        return fmaxf(m, fmaf(kg_max(mx), f, (float)ev));
+        return fmaxf(m, fmaf(kg_max(mx), f, (float)(ev - kQ8TopBits)));
       };
       auto weigh = [&] {
         const float off = (float)ev - m;
-        sum = 0.f;
+        float part[2] = {0.f, 0.f};
 #pragma unroll
         for (int y = 0; y < 8; ++y) {
           const q8_f32x2 p = {__builtin_amdgcn_exp2f(fmaf(s[y >> 1][2 * (y & 1)], f, off)), __builtin_amdgcn_exp2f(fmaf(s[y >> 1][2 * (y & 1) + 1], f, off))};
-          sum += p[0] + p[1];
           w[y] = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, q8_f16x2));
+          part[y & 1] = q8_add2(w[y], part[y & 1]);
         }
+        sum = part[0] + part[1];
       };
       if (fresh) raise(largest());
       fresh = false;

@@ -30,6 +30,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kRows = 128;     // query rows of a workgroup
 constexpr int kMinTiles = 4;   // tiles of a piece, at least (37 tokens over 777 rows 44.3 us; with 2 43.8, with 6 46, with 8 49.4; over 8000 alike)
 constexpr int kMaxSplit = 32;
+constexpr int kPageBits = 6;   // a page's values are made as large as those of this call's tiles (codes below 2^9, tiles below 2^15)
 
 struct pf_args {
   const uint16_t *q, *k, *v;
@@ -159,7 +160,7 @@ __global__ __launch_bounds__(256, 2) void ag_q8_prefill_kernel(pf_args a) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(o[dt][i]) < INFINITY ? fabsf(o[dt][i]) : 0.f);
     top = fmaxf(top, other_half(top));
-    int e = max(kQ8TileMinExp, max(1, (int)(__float_as_uint(top) >> 23)) - 127 - kQ8TileTop);
+    int e = max(kQ8TileMinExp, max(1, (int)(__float_as_uint(top) >> 23)) - 127 - kQ8TileTop) - kQ8TopBits;
     // seeing nothing else its weight is 1 whatever its score is; a score that overflowed to -infinity counts as the least number
     if (meta.blocks == 0 && bound == 0) s = 0.f, e = 0;
     m = (s < kQ8EmptyMax ? kQ8EmptyMax : s) + (float)e;
@@ -185,7 +186,7 @@ __global__ __launch_bounds__(256, 2) void ag_q8_prefill_kernel(pf_args a) {
   // Lane x knows tile w_first + x: its page (0: a tile of this call; -1: not there, or odd) and its exponents.  (Read tile by tile, the
   // page's number and then its scales would be waited for in every step.)
   int w_first = t0, w_id = -1, w_ek = 0, w_ev = 0;
-  bool any_odd = false;
+  bool any_odd = false, fresh = true;  // fresh: no tile has been taken yet
   auto look_up = [&](int first) {
     const int t = first + lane;
     bool odd = false;
@@ -196,7 +197,7 @@ __global__ __launch_bounds__(256, 2) void ag_q8_prefill_kernel(pf_args a) {
       const int p = page[t], ps = (uint32_t)p < (uint32_t)a.c.n_pages ? p : 0;  // (a page number outside the pool counts as evicted rows)
       w_id = ps == p ? p : -1;
       w_ek = (int)(__float_as_uint(a.c.k_scale[ps]) >> 23) - 127;
-      w_ev = (int)(__float_as_uint(a.c.v_scale[ps]) >> 23) - 127;
+      w_ev = (int)(__float_as_uint(a.c.v_scale[ps]) >> 23) - 127 - kPageBits;
     } else if (t < t1) {
       const q8_tile_info info = q8_tile_of(a.info[(size_t)u * a.n_blk + t - meta.blocks]);
       odd = info.odd;
@@ -247,7 +248,7 @@ __global__ __launch_bounds__(256, 2) void ag_q8_prefill_kernel(pf_args a) {
     }
     if (D == 128 || tid < 128) {
       const int e = __builtin_amdgcn_readlane(w_ev, t - w_first);
-      const float scale = q8_pow2(e - max(kQ8TileMinExp, e));
+      const float scale = q8_pow2(e + kPageBits - max(kQ8TileMinExp, e));
       const uint32_t lo[4] = {rv[0].x, rv[0].y, rv[0].z, rv[0].w}, hi[4] = {rv[1].x, rv[1].y, rv[1].z, rv[1].w};
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -289,8 +290,9 @@ __global__ __launch_bounds__(256, 2) void ag_q8_prefill_kernel(pf_args a) {
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
         if (x + 4 < 2 * KS) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
       }
-      // s[x][i]: row 32 x + 8 (i / 4) + 4 h + i % 4 of the tile.  The state is kept relative to m, the largest score plus its tile's ev: a
-      // tile's weights are 2^(score + ev - m), at most 2^15, its values v 2^-ev, and its part of the row sum is 2^-ev the sum of its weights.
+      // s[x][i]: row 32 x + 8 (i / 4) + 4 h + i % 4 of the tile.  The state is kept relative to m, the largest score plus its tile's ev less
+      // kQ8TopBits: a tile's weights are 2^(score + ev - m), at most 2^15, its values v 2^-ev, and its part of the row sum is 2^-ev the sum of
+      // its weights, as the second product takes them: what rounding them changes cancels.
       const float f = fmaxf(ldexpf(a.qscale, eq + ek), 1.17549435e-38f), ev = (float)e_v;
       if (t >= meta.blocks && first + kQ8Block > see_all) {
         const int b = bound - first - 4 * h;
@@ -301,7 +303,7 @@ __global__ __launch_bounds__(256, 2) void ag_q8_prefill_kernel(pf_args a) {
             if (32 * x + 8 * (i / 4) + i % 4 >= b) s[x][i] = -INFINITY;
       }
       uint32_t p[2][8];
-      float sum;
+      float sum = 0.f;
       auto weigh = [&] {
         const float off = ev - m;
         float part[2] = {0.f, 0.f};
@@ -310,28 +312,28 @@ __global__ __launch_bounds__(256, 2) void ag_q8_prefill_kernel(pf_args a) {
 #pragma unroll
           for (int i = 0; i < 16; i += 2) {
             const q8_f32x2 w = {__builtin_amdgcn_exp2f(fmaf(s[x][i], f, off)), __builtin_amdgcn_exp2f(fmaf(s[x][i + 1], f, off))};
-            part[0] += w[0];
-            part[1] += w[1];
             p[x][i / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(w, q8_f16x2));
             asm volatile("" : "+v"(p[x][i / 2]));  // (packed here: the compiler would carry all 32 weights to the second product)
+            part[i / 2 & 1] = q8_add2(p[x][i / 2], part[i / 2 & 1]);
           }
         sum = part[0] + part[1];
       };
-      weigh();
-      if (__any(!(sum <= 32768.f))) {  // the reference is too far below (or nothing yet): a new one, and the weights again
+      if (!fresh) weigh();
+      if (fresh || __any(!(sum <= 32768.f))) {  // no reference yet, or too far below: a new one, and the weights again
         float mx = -INFINITY;
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
           for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[x][i]);
-        mx = fmaf(fmaxf(mx, other_half(mx)), f, ev);
+        mx = fmaf(fmaxf(mx, other_half(mx)), f, ev - (float)kQ8TopBits);
         const float both = fmaxf(sum <= 32768.f ? 0.f : 1.f, other_half(sum <= 32768.f ? 0.f : 1.f));
-        const float m_new = both > 0.f ? fmaxf(m, mx) : m;  // (a row's own reference alone: no row depends on its neighbours)
+        const float m_new = fresh || both > 0.f ? fmaxf(m, mx) : m;  // (a row's own reference alone: no row depends on its neighbours)
         const float alpha = __builtin_amdgcn_exp2f(m - m_new);
         l *= alpha;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) o[dt] *= alpha;
         m = m_new;
+        fresh = false;
         weigh();
       }
       l += ldexpf(sum, -e_v);

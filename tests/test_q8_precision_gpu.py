@@ -129,3 +129,34 @@ def test_steps_whose_new_token_has_half_of_the_weight_at_large_scores(B, H, G, D
     assert step_error(ref, gen(5), q, k, v, torch.ones(B, H, dtype=torch.uint8), scale, 1).max() <= bar(spread)
 
 
+
+
+# ------------------------------------------------------------------------------------------------------------ many small weights
+@pytest.mark.parametrize("rows,bits", [(300000, 25.5), (400000, 24.5), (64 * 3000, 22.3)])
+def test_many_small_weights_are_not_lost(rows, bits):
+    """One row that every query sees with a score of bits ln 2, and so many with a score of 0 that they make 0.6 to 4 % of the sum: in closed
+    form, as all of these are alike."""
+    g, H, G, D, L = gen(rows), 8, 8, 128, 512       # (so many query rows that no row's keys are cut into pieces)
+    blocks, scale, low = rows // 64, D ** -0.5, 2.0
+    sign = torch.randint(0, 2, (D,), generator=g).float() * 2 - 1
+    value = torch.randn(D, generator=g).to(torch.float8_e4m3fn).float()
+    keys, values = torch.zeros(2, 64 * D), torch.full((2, 64 * D), low)
+    keys[0, R.places(D)[0][7]], values[0, R.places(D)[1][7]] = sign, value           # row 7 of page 0, which is every unit's first one
+    page = torch.ones(H, blocks + L // 64 + 1, dtype=torch.int32)
+    page[:, 0] = 0
+    pools = [x.to(torch.float8_e4m3fn).view(torch.uint8).to(DEV) for x in (keys, values)]
+    tails = [torch.zeros(H, 64 * D, dtype=BF, device=DEV) for _ in range(2)]
+    cache = ag.Q8Cache(*pools, torch.ones(2, device=DEV), torch.ones(2, device=DEV), *tails, page.to(DEV),
+                       torch.full((H,), blocks * 64, dtype=torch.int32, device=DEV), 1, H, D)
+    q = (sign * (bits * 0.6931471805599453 / scale / D) + 0.02 * torch.randn(1, H * G, L, D, generator=g)).to(BF)
+    k, v = (-sign).expand(1, H, L, D).to(BF).contiguous(), some(g, 1, H, L, D)        # evicted, and their own scores are the least
+    ctx, out = ag.Context(0, ag.q8_workspace_bytes(1, L, H * G, H, D, blocks + L // 64 + 1)), torch.empty_like(q, device=DEV)
+    print("turn", rows, bits, flush=True)
+    ag.ag_q8_prefill_attn(ctx, q.to(DEV), k.to(DEV), v.to(DEV), torch.zeros(1, H, L, dtype=torch.uint8, device=DEV), None, scale, cache, out)
+    ctx.poll_error()
+    own = (q.double() * k.double().repeat_interleave(G, dim=1)).sum(-1, keepdim=True) * scale
+    score = (q.double() @ sign.double())[..., None] * scale
+    w, w_own = torch.exp(-score) * (blocks * 64 - 1), torch.exp(own - score)
+    e = row_errors(out, (value.double() + w * low + w_own * v.double().repeat_interleave(G, dim=1)) / (1 + w + w_own))
+    print("turn", rows, bits, "row errors: mean %.2e, worst %.2e" % (e.mean().item(), e.max().item()), flush=True)
+    assert e.max() <= bar()
