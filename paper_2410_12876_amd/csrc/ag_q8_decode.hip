@@ -35,6 +35,9 @@ constexpr int kFewUnits = 128;
 // 19.4).
 constexpr int kWholeRounds = 2;
 constexpr int kValueBits = 9;     // a page's values in f16 are below 1 (exact: a code has 4 bits, the least is 2^-9), as the tail's are of unit size
+// Bits by which a page's reference may lie below the one that a tail has left: its weights are then 2^-4 at most, and those down to 2^-21 of
+// the largest count.  (Values of unit size: 5.  Coming down costs a step of few rows 0.4 us of 9.6.)
+constexpr float kHighBits = kQ8TopBits + 4;
 constexpr int kArriveSplit = 64;  // workgroups from which their arrivals are counted at several addresses
 // What a unit costs a workgroup beside its items, in items, where all units are cut into equal ranges: the start of a segment, the tail's two
 // bytes a value, the merge.  Without it the ranges that hold the most units end last (a step with 0, 7, 14, 28: 128 units of 8000 rows 41.5,
@@ -164,6 +167,30 @@ template <int D, int G> struct wave_q8 {
     }
   }
 
+  // How far the reference may come down: the state grows by as much, and must not overflow (what is not finite already stays so).
+  __device__ __forceinline__ float lower() const {
+    float top[4];  // (the larger of three magnitudes an instruction; four chains, or every one would wait for the one before it)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      top[r] = fabsf(o[0][r]);
+#pragma unroll
+      for (int f = 1; f < VF; f += 2) {
+        const float x = o[f][r], y = o[f + 1 < VF ? f + 1 : f][r];
+        asm("v_max3_f32 %0, %0, |%1|, |%2|" : "+v"(top[r]) : "v"(x), "v"(y));
+      }
+    }
+    if (!__any(!(top[0] < 0x1p59f) | !(top[1] < 0x1p59f) | !(top[2] < 0x1p59f) | !(top[3] < 0x1p59f))) return -(float)kQ8TileMinExp;
+    uint32_t most = 0;
+#pragma unroll
+    for (int f = 0; f < VF; ++f)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const uint32_t x = __float_as_uint(o[f][r]) & 0x7fffffffu;
+        most = max(most, x < 0x7f800000u ? x : 0u);
+      }
+    return (float)max(0, min(-kQ8TileMinExp, 127 + 120 - (int)(wave_max(most) >> 23)));
+  }
+
   // A wave's pages: lane x holds the number and the exponents of its page x (of at most 64 at a time); two pages are in flight.
   int ids, ek_v, ev_v;
   // (The same registers hold a tail instead: as long as the two were told apart the compiler kept room for both.)
@@ -219,7 +246,7 @@ template <int D, int G> struct wave_q8 {
         float mx = s[0][0];
 #pragma unroll
         for (int y = 1; y < 16; ++y) mx = fmaxf(mx, s[y >> 2][y & 3]);
-        return fmaxf(m, fmaf(kg_max(mx), f, (float)(ev - kQ8TopBits)));
+        return fmaf(kg_max(mx), f, (float)(ev - kQ8TopBits));
       };
       auto weigh = [&] {
         const float off = (float)ev - m;
@@ -232,12 +259,17 @@ template <int D, int G> struct wave_q8 {
         }
         sum = part[0] + part[1];
       };
-      if (fresh) raise(largest());
+      if (fresh) {
+        // The wave's first page.  The reference that a tail has left is a score without an exponent: where the values are small it is too high
+        // for a page's weights in f16, and comes down (the state is in 32 bits).
+        const float mx = largest();
+        raise(fmaxf(mx, __builtin_expect(__any(mx < m - kHighBits), 0) ? m - lower() : m));
+      }
       fresh = false;
       weigh();
       // no maximum in the common case: only where weights pass 2^15 is the reference moved (for that head alone)
       if (__any(!(sum <= 32768.f))) {
-        const float m_new = largest();
+        const float m_new = fmaxf(m, largest());
         raise(kg_max(sum <= 32768.f ? 0.f : 1.f) > 0.f ? m_new : m);
         weigh();
       }

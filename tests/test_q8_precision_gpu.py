@@ -129,6 +129,25 @@ def test_steps_whose_new_token_has_half_of_the_weight_at_large_scores(B, H, G, D
     assert step_error(ref, gen(5), q, k, v, torch.ones(B, H, dtype=torch.uint8), scale, 1).max() <= bar(spread)
 
 
+@pytest.mark.parametrize("values", [0, -6, -10, -20, 20])
+@pytest.mark.parametrize("B,H,G,D,longest", [(1, 8, 4, 128, 3000), (2, 3, 1, 64, 800), (130, 10, 1, 64, 320), (65, 4, 2, 64, 900)])
+def test_steps_over_values_of_any_size(B, H, G, D, longest, values):
+    """Eight waves a unit, one wave a unit, units in equal ranges: a wave has the tail and pages behind it."""
+    g = gen(values + D + longest)
+    ref = many_units(B, H, D, longest, g, values)
+    q, k, v, f = some(g, B, H * G, D), some(g, B, H, D), some(g, B, H, D) * 2.0 ** values, flags_of(g, "rand", B, H, 1)[:, :, 0].contiguous()
+    assert step_error(ref, g, q, k, v, f, D ** -0.5, 1).max() <= bar()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_steps_whose_tail_and_pages_hold_values_of_different_sizes(D):
+    g, H = gen(D + 9), 8
+    for pages, tail in ((-12, 0), (0, -12), (30, 0), (0, 30), (90, -20), (-20, 90), (40, 90)):
+        ref = many_units(1, H, D, 500, g)
+        ref.scales[1] *= 2.0 ** pages
+        ref.tails[1] *= 2.0 ** tail
+        q, k, v = some(g, 1, H, D), some(g, 1, H, D), some(g, 1, H, D) * 2.0 ** tail
+        assert step_error(ref, g, q, k, v, torch.zeros(1, H, dtype=torch.uint8), D ** -0.5).max() <= bar()
 
 
 # ------------------------------------------------------------------------------------------------------------ many small weights
