@@ -331,7 +331,8 @@ typedef struct {
   int32_t B, Hkv, D;
 } ag_q8_cache;
 
-/* Workspace that covers the calls below (L = 1: ag_q8_decode_attn) on one cache; Hq = Hkv will do for ag_q8_append alone. */
+/* Workspace that covers the calls below on one cache, with up to L tokens each (L = 1: ag_q8_decode_attn); Hq = Hkv will do for
+ * ag_q8_append alone. */
 size_t ag_q8_workspace_bytes(int B, int L, int Hq, int Hkv, int D, int max_blocks);
 
 /*

@@ -70,6 +70,8 @@ struct ag_q8_prefill_ws {
   int n_qt, n_split;    // query tiles of a unit; pieces a query tile's work may be cut into
 };
 void ag_q8_prefill_plan(int num_cu, int U, int Hq, int Hkv, int L, int D, int max_blocks, ws_cursor &ws, ag_q8_prefill_ws *w);
+// The longest call of fewer query tiles than one of L tokens has (0: there is none).  Of calls with equally many the longest needs most.
+int ag_q8_prefill_shorter(int Hq, int Hkv, int L);
 hipError_t ag_launch_q8_prefill(ag_ctx *ctx, hipStream_t s, const void *q, const void *k, const void *v, int B, int Hq, int Hkv, int L,
                                 int D, const uint64_t *words, const int32_t *blk_off, const ag_rope_dev &rope, float scale,
                                 const ag_q8_dev &cache, const ag_q8_prefill_ws &w, void *out);

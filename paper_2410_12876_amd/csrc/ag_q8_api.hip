@@ -7,7 +7,7 @@
 
 namespace {
 
-constexpr int kMostCu = 1024;  // upper bound on the CUs of a device, for sizes that are asked for without one
+constexpr int kMostCu = 256;  // CUs of a gfx950, at most: for sizes that are asked for without a device
 
 bool aligned(std::initializer_list<const void *> p) {
   return std::all_of(p.begin(), p.end(), [](const void *x) { return ((uintptr_t)x & 15) == 0; });
@@ -97,14 +97,13 @@ ag_status ag_rotate(ag_ctx *ctx, void *hip_stream, const void *q, const void *k,
 size_t ag_q8_workspace_bytes(int B, int L, int Hq, int Hkv, int D, int max_blocks) {
   if (B <= 0 || L <= 0 || (D != 128 && D != 64) || max_blocks <= 0 || !group_ok(Hq, Hkv) || (int64_t)B * Hkv > kDecodeMaxUnits || L > kMaxL) return 0;
   const int units = B * Hkv;
-  ws_cursor count{nullptr, ~size_t(0) >> 1, 0, true};
   static const uint8_t some = 0;
-  take_scan(count, &some, units, L);
   size_t most = 0;
-  for (int cu = 1; cu <= kMostCu; cu *= 2) {  // (the cut depends on the device: the most that any needs)
-    ws_cursor ws = count;
+  for (int l = L; l > 0; l = ag_q8_prefill_shorter(Hq, Hkv, l)) {  // (shorter calls are cut into more pieces: the most that any needs)
+    ws_cursor ws{nullptr, ~size_t(0) >> 1, 0, true};
+    take_scan(ws, &some, units, l);
     ag_q8_prefill_ws w;
-    ag_q8_prefill_plan(cu, units, Hq, Hkv, L, D, max_blocks, ws, &w);
+    ag_q8_prefill_plan(kMostCu, units, Hq, Hkv, l, D, max_blocks, ws, &w);
     most = std::max(most, ws.off);
   }
   return std::max(most, ag_align256(ag_ws_q8_decode_floats(kMostCu, Hq / Hkv, D) * sizeof(float))) + 4096;

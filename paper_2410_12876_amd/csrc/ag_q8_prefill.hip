@@ -487,6 +487,11 @@ void ag_q8_prefill_plan(int num_cu, int U, int Hq, int Hkv, int L, int D, int ma
   w->part = w->n_split > 1 ? ws.take<float>((size_t)U * w->n_qt * w->n_split * kRows * (D + 4)) : nullptr;
 }
 
+int ag_q8_prefill_shorter(int Hq, int Hkv, int L) {
+  const int G = Hq / Hkv;
+  return (int)((((int64_t)L * G + kRows - 1) / kRows - 1) * kRows / G);
+}
+
 hipError_t ag_launch_q8_prefill(ag_ctx *ctx, hipStream_t s, const void *q, const void *k, const void *v, int B, int Hq, int Hkv, int L,
                                 int D, const uint64_t *words, const int32_t *blk_off, const ag_rope_dev &rope, float scale,
                                 const ag_q8_dev &cache, const ag_q8_prefill_ws &w, void *out) {
