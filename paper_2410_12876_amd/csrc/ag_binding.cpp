@@ -254,6 +254,16 @@ AG_BINDING(gate_mha, 10) {
   return call([&] { return ag_gate_mha(ctx, s, xp, dt, B, L, d, w, hp, dp, wop, bias, H, tau, n_sink, logits, flags); });
 }
 
+void like(const at::Tensor &t, const at::Tensor &other, const char *msg) {
+  if (t.scalar_type() != other.scalar_type() || t.sizes() != other.sizes()) fail(PyExc_ValueError, msg);
+}
+// One byte for each of a call's n tokens of the units, or None.
+const uint8_t *flags_of(PyObject *o, int64_t n) {
+  if (THPVariable_Check(o) && (tensor(o).element_size() != 1 || tensor(o).numel() != n))
+    fail(PyExc_ValueError, "flags are not one byte for every token of every KV head");
+  return ptr_as<uint8_t>(o);
+}
+
 // q, k, rope, q_out, k_out
 AG_BINDING(rotate, 5) {
   const at::Tensor &q = tensor(a[0]);
@@ -264,7 +274,9 @@ AG_BINDING(rotate, 5) {
     Hkv = dim(k, 4, 1);
     if (k.scalar_type() != q.scalar_type() || k.size(0) != B || k.size(2) != L || k.size(3) != D)
       fail(PyExc_ValueError, "rotate: q and k differ in more than their heads");
+    if (THPVariable_Check(a[4])) like(tensor(a[4]), k, "rotate: k_out and k differ");
   }
+  if (THPVariable_Check(a[3])) like(tensor(a[3]), q, "rotate: q_out and q differ");
   const ag_dtype dt = dtype_of(q);
   const void *qp = ptr(a[0]), *k = ptr(a[1]);
   const ag_rope *r = struct_of<ag_rope>(a[2]);
@@ -278,9 +290,6 @@ void like_cache(const at::Tensor &t, const ag_q8_cache *c, int dims) {
   if (c && (dim(t, dims, 0) != c->B || t.size(1) != c->Hkv || t.size(dims - 1) != c->D))
     fail(PyExc_ValueError, "a tensor's shape differs from the cache's");
 }
-void like(const at::Tensor &t, const at::Tensor &other, const char *msg) {
-  if (t.scalar_type() != other.scalar_type() || t.sizes() != other.sizes()) fail(PyExc_ValueError, msg);
-}
 
 // k, v, flags, rope, cache
 AG_BINDING(q8_append, 5) {
@@ -291,7 +300,7 @@ AG_BINDING(q8_append, 5) {
   like_cache(k, c, 4);
   like(tensor(a[1]), k, "k and v differ");
   const void *kp = ptr(a[0]), *v = ptr(a[1]);
-  const uint8_t *f = ptr_as<uint8_t>(a[2]);
+  const uint8_t *f = flags_of(a[2], k.size(0) * k.size(1) * L);
   return call([&] { return ag_q8_append(ctx, s, kp, v, f, L, r, c); });
 }
 
@@ -308,7 +317,7 @@ AG_BINDING(q8_prefill_attn, 8) {
   if (q.scalar_type() != k.scalar_type() || q.size(0) != k.size(0) || k.size(2) != L || q.size(3) != k.size(3))
     fail(PyExc_ValueError, "q and k differ in more than their heads");
   const void *qp = ptr(a[0]), *kp = ptr(a[1]), *v = ptr(a[2]);
-  const uint8_t *f = ptr_as<uint8_t>(a[3]);
+  const uint8_t *f = flags_of(a[3], k.size(0) * k.size(1) * L);
   void *out = ptr(a[7]);
   return call([&] { return ag_q8_prefill_attn(ctx, s, qp, kp, v, f, L, Hq, r, scale, c, out); });
 }
@@ -326,7 +335,7 @@ AG_BINDING(q8_decode_attn, 8) {
   if (q.scalar_type() != k.scalar_type() || q.size(0) != k.size(0) || q.size(2) != k.size(2))
     fail(PyExc_ValueError, "q and k_new differ in more than their heads");
   const void *qp = ptr(a[0]), *kp = ptr(a[1]), *v = ptr(a[2]);
-  const uint8_t *f = ptr_as<uint8_t>(a[3]);
+  const uint8_t *f = flags_of(a[3], k.size(0) * k.size(1));
   void *out = ptr(a[7]);
   return call([&] { return ag_q8_decode_attn(ctx, s, qp, kp, v, f, Hq, r, scale, c, out); });
 }

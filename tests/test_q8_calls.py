@@ -22,3 +22,28 @@ def test_a_workspace_covers_shorter_calls(lib, B, Hq, Hkv, D, L, blocks):  # noq
         expect(ag.AG_EHIP, ag.ag_q8_append, ctx, of(B, Hkv, n, D), of(B, Hkv, n, D), f, None, c, stream=0)
     expect(ag.AG_EHIP, ag.ag_q8_decode_attn, ctx, of(B, Hq, D), of(B, Hkv, D), of(B, Hkv, D), None, None, 0.1, c, of(B, Hq, D), stream=0)
     ctx.close()
+
+
+def test_flags_and_outputs_of_another_size_or_type_are_refused(lib):  # noqa: F811
+    ctx = ag.Context(device=-1, workspace=ag.q8_workspace_bytes(1, 8, 4, 2, 64, 3))
+    q, k, c = torch.zeros(1, 4, 8, 64, dtype=BF), torch.zeros(1, 2, 8, 64, dtype=BF), cache()
+    r = ag.Rope(torch.zeros(20, 64), torch.zeros(1, 1, 8, dtype=torch.int32))
+    one = lambda x: x[:, :, 0].contiguous()  # noqa: E731
+    turn = lambda f: ag.ag_q8_prefill_attn(ctx, q, k, k, f, None, 0.1, c, q.clone(), stream=0)  # noqa: E731
+    append = lambda f: ag.ag_q8_append(ctx, k, k, f, None, c, stream=0)  # noqa: E731
+    step = lambda f: ag.ag_q8_decode_attn(ctx, one(q), one(k), one(k), f, None, 0.1, c, one(q), stream=0)  # noqa: E731
+    for call, shape in ((turn, (1, 2, 8)), (append, (1, 2, 8)), (step, (1, 2))):
+        for good in (torch.zeros(shape, dtype=torch.uint8), torch.zeros(shape, dtype=torch.bool), None):
+            expect(ag.AG_EHIP, call, good)
+        for bad in (torch.zeros(shape, dtype=torch.int32), torch.zeros(shape, dtype=BF), torch.zeros(shape[:-1] + (shape[-1] - 1,), dtype=torch.uint8),
+                    torch.zeros((2,) + shape[1:], dtype=torch.uint8)):
+            with pytest.raises(ValueError):
+                call(bad)
+    expect(ag.AG_EHIP, ag.ag_rotate, ctx, q, k, r, q, k.clone(), stream=0)
+    expect(ag.AG_EHIP, ag.ag_rotate, ctx, q, None, r, q.clone(), None, stream=0)
+    for q_out, k_out in ((q[:, :, :7].contiguous(), k), (q.float(), k), (q, k[:, :1].contiguous()), (q, k.float())):
+        with pytest.raises(ValueError):
+            ag.ag_rotate(ctx, q, k, r, q_out, k_out, stream=0)
+    with pytest.raises(ValueError):
+        ag.ag_rotate(ctx, q.float(), None, ag.Rope(r.table, r.pos), q, None, stream=0)
+    ctx.close()
