@@ -105,7 +105,8 @@ __global__ __launch_bounds__(256, 2) void ag_q8_prefill_kernel(pf_args a) {
   const size_t k_at = ((size_t)u * a.L + j) * D;
   bool kept;
   const int rank = rank_of(a, u, j, meta.added, kept);
-  const int bound = meta.held + rank + (kept ? 1 : 0);  // visible rows of those tiles
+  const bool sole = meta.blocks == 0 && meta.held + rank == 0;  // it sees nothing else
+  const int bound = sole ? 0 : meta.held + rank + (kept ? 1 : 0);  // visible rows of those tiles
   // The query in f16 times 2^eq (11 bits; bf16 would lose up to 2^-9 of a turned value, and the scores as much of themselves)
   q8_rows at = {0, 0, 0};
   auto angles = [&](int i) { return q8_angles4(a.rope, at, i, D); };
@@ -133,7 +134,7 @@ __global__ __launch_bounds__(256, 2) void ag_q8_prefill_kernel(pf_args a) {
     for (int ks = 0; ks < KS; ++ks) qx[ks] = y[ks].f16(inv);
   }
   float m = kQ8EmptyMax, l = 0.f;
-  const bool alone = piece == 0 && !kept;  // an evicted token sees itself
+  const bool alone = piece == 0 && (!kept || sole);  // an evicted token sees itself, and so does a kept one that sees nothing else
   q8_f32x16 o[DT];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
@@ -162,7 +163,7 @@ __global__ __launch_bounds__(256, 2) void ag_q8_prefill_kernel(pf_args a) {
     top = fmaxf(top, other_half(top));
     int e = max(kQ8TileMinExp, max(1, (int)(__float_as_uint(top) >> 23)) - 127 - kQ8TileTop) - kQ8TopBits;
     // seeing nothing else its weight is 1 whatever its score is; a score that overflowed to -infinity counts as the least number
-    if (meta.blocks == 0 && bound == 0) s = 0.f, e = 0;
+    if (sole) s = 0.f, e = 0;
     m = (s < kQ8EmptyMax ? kQ8EmptyMax : s) + (float)e;
     const float scale = q8_pow2(-e);
     l = h == 0 ? scale : 0.f;  // (summed over the halves at the end)
