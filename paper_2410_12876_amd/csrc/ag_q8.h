@@ -194,6 +194,9 @@ __device__ __forceinline__ float q8_turn(float x, float p, float c, float s, boo
   const float a = x * c, b = p * s;
   return lower ? a - b : a + b;
 }
+// What products of numbers 2^-e as large are multiplied by: scale 2^e, but neither 0 nor infinite, so that a product of 0 stays 0 and one that
+// is infinite an infinity.
+__device__ __forceinline__ float q8_unscale(float scale, int e) { return __builtin_amdgcn_fmed3f(ldexpf(scale, e), 1.17549435e-38f, 3.40282347e+38f); }
 // The two f16 of a word added to x.
 __device__ __forceinline__ float q8_add2(uint32_t w, float x) {
   const q8_f16x2 one = {(_Float16)1.f, (_Float16)1.f};

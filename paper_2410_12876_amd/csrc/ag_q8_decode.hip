@@ -239,7 +239,7 @@ template <int D, int G> struct wave_q8 {
     if (more) load<B * KF>(c.k, x + 2);
     if (now) {
       const int e = __builtin_amdgcn_readlane(ev_v, x), ev = max(kQ8TileMinExp, e + kValueBits);
-      const float f = fmaxf(ldexpf(qscale, eq + __builtin_amdgcn_readlane(ek_v, x)), 1.17549435e-38f);
+      const float f = q8_unscale(qscale, eq + __builtin_amdgcn_readlane(ek_v, x));
       float sum;
       uint32_t w[8];
       auto largest = [&] {
@@ -383,7 +383,7 @@ template <int D, int G> struct wave_q8 {
         }
         s_new = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(q8_bf16x8, nl[c][h]), qh, s_new, 0, 0, 0);
       }
-    const float f = fmaxf(ldexpf(a.qscale, eq), 1.17549435e-38f);
+    const float f = q8_unscale(a.qscale, eq);
     float mx = -INFINITY;
 #pragma unroll
     for (int x = 0; x < 4; ++x)

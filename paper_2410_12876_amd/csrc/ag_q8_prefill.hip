@@ -153,7 +153,7 @@ __global__ __launch_bounds__(256, 2) void ag_q8_prefill_kernel(pf_args a) {
     for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
       for (int i = 0; i < 4; ++i) s = fmaf((float)qx[ks][i], y[ks].a[i], fmaf((float)qx[ks][4 + i], y[ks].b[i], s));
-    s = (s + other_half(s)) * ldexpf(a.qscale, eq);
+    s = (s + other_half(s)) * q8_unscale(a.qscale, eq);
     // Its value has an exponent as a tile has one: the reference is the score plus that, or the tiles' weights would be as much too small
     // for f16 as the values are small.  (Values that are not finite do not count: other columns are not theirs.)
 #pragma unroll
@@ -294,7 +294,7 @@ __global__ __launch_bounds__(256, 2) void ag_q8_prefill_kernel(pf_args a) {
       // s[x][i]: row 32 x + 8 (i / 4) + 4 h + i % 4 of the tile.  The state is kept relative to m, the largest score plus its tile's ev less
       // kQ8TopBits: a tile's weights are 2^(score + ev - m), at most 2^15, its values v 2^-ev, and its part of the row sum is 2^-ev the sum of
       // its weights, as the second product takes them: what rounding them changes cancels.
-      const float f = fmaxf(ldexpf(a.qscale, eq + ek), 1.17549435e-38f), ev = (float)e_v;
+      const float f = q8_unscale(a.qscale, eq + ek), ev = (float)e_v;
       if (t >= meta.blocks && first + kQ8Block > see_all) {
         const int b = bound - first - 4 * h;
 #pragma unroll
@@ -355,7 +355,7 @@ __global__ __launch_bounds__(256, 2) void ag_q8_prefill_kernel(pf_args a) {
     if (t + 1 < t1) stage(t + 1, buf ^ 1);
   }
   if (any_odd) {  // rare: tiles with values that are not finite, or of too different sizes; row by row in 32 bits
-    const float f = ldexpf(a.qscale, eq);
+    const float f = q8_unscale(a.qscale, eq);
     for (int t = max(t0, meta.blocks); t < t1; ++t) {
       const int first = (t - meta.blocks) * kQ8Block;
       if (!q8_tile_of(a.info[(size_t)u * a.n_blk + t - meta.blocks]).odd) continue;
