@@ -90,7 +90,7 @@ const char *ag_last_error(const ag_ctx *ctx);
 size_t ag_workspace_bytes(int B, int L, int Hq, int Hkv, int D, ag_dtype dtype, int d_in, int64_t cache_rows);
 
 /* Synchronise `stream`, read and clear the sticky device error word.  AG_OK, AG_ECAPACITY, or AG_EINVAL (a position outside
- * the table of an ag_rope).
+ * the table of an ag_rope); where both have happened, one call reports AG_ECAPACITY and the next one AG_EINVAL.
  * (Kernel timing and machine probes for benchmarks are declared in ag_bench.h; they are no part of the method.) */
 ag_status ag_poll_error(ag_ctx *ctx, void *hip_stream);
 

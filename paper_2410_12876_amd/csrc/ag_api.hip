@@ -196,7 +196,8 @@ ag_status ag_poll_error(ag_ctx *ctx, void *hip_stream) {
   AG_HIP(hipMemcpyAsync(&h, ctx->d_err, sizeof(h), hipMemcpyDeviceToHost, (hipStream_t)hip_stream));
   AG_HIP(hipStreamSynchronize((hipStream_t)hip_stream));
   if (h) {
-    AG_HIP(hipMemsetAsync(ctx->d_err, 0, sizeof(h), (hipStream_t)hip_stream));
+    const int32_t left = h & 1 ? h & ~1 : 0;  // one error a call
+    AG_HIP(hipMemsetD32Async((hipDeviceptr_t)ctx->d_err, left, 1, (hipStream_t)hip_stream));
     AG_HIP(hipStreamSynchronize((hipStream_t)hip_stream));
     if (h & 1) return ag_fail(ctx, AG_ECAPACITY, "a cache unit overflowed its capacity; the extra rows were dropped");
     return ag_fail(ctx, AG_EINVAL, "a position lies outside the rotation table; the nearest row was used");
