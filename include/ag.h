@@ -354,7 +354,7 @@ ag_status ag_q8_prefill_attn(ag_ctx *ctx, void *hip_stream, const void *q, const
 
 /*
  * One decoding step: the same with L = 1, in one launch.  q, out [B, Hq, D]; k_new, v_new [B, Hkv, D]; new_flags uint8 [B, Hkv] or
- * NULL; rope->pos [n_axes, B, 1].
+ * NULL; rope->pos [n_axes, B, 1].  B * Hkv * (max_blocks + 15) must stay below 2^31 - 2^16.
  */
 ag_status ag_q8_decode_attn(ag_ctx *ctx, void *hip_stream, const void *q, const void *k_new, const void *v_new,
                             const uint8_t *new_flags, int Hq, const ag_rope *rope, float scale, ag_q8_cache *cache, void *out);

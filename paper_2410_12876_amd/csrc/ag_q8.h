@@ -59,6 +59,7 @@ hipError_t ag_launch_q8_fill(ag_ctx *ctx, hipStream_t s, const void *k, const vo
                              uint64_t *words, int32_t *blk_off, const ag_rope_dev &rope, const ag_q8_dev &cache,
                              uint16_t *tiles, uint32_t *info, ag_q8_meta *meta);
 size_t ag_ws_q8_decode_floats(int num_cu, int G, int D);  // records of a step
+int64_t ag_q8_decode_cost(int64_t units, int max_blocks);  // the largest number that a step's work list can come to; it counts in 32 bits
 hipError_t ag_launch_q8_decode(ag_ctx *ctx, hipStream_t s, const void *q, const void *k_new, const void *v_new, const uint8_t *new_flags,
                                int B, int Hq, int Hkv, int D, const ag_rope_dev &rope, float scale, const ag_q8_dev &cache, void *out, float *rec);
 

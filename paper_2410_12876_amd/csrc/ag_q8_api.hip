@@ -175,6 +175,8 @@ ag_status ag_q8_decode_attn(ag_ctx *ctx, void *hip_stream, const void *q, const 
   AG_REQUIRE(Hq > 0 && Hq % cache->Hkv == 0, AG_EINVAL, "ag_q8_decode_attn: Hq must be a positive multiple of Hkv");
   AG_REQUIRE(group_ok(Hq, cache->Hkv), AG_EUNSUPPORTED, "ag_q8_decode_attn: %d query heads per KV head", Hq / cache->Hkv);
   AG_REQUIRE(aligned({q, k_new, v_new, out}), AG_EINVAL, "ag_q8_decode_attn: tensors must be 16-byte aligned");
+  AG_REQUIRE(ag_q8_decode_cost((int64_t)cache->B * cache->Hkv, cache->max_blocks) < (1ll << 31), AG_EUNSUPPORTED,
+             "ag_q8_decode_attn: cache: %d units of max_blocks = %d are too many", cache->B * cache->Hkv, cache->max_blocks);
   ag_rope_dev r;
   st = check_rope(ctx, "ag_q8_decode_attn", rope, cache->D, cache->B, &r);
   if (st != AG_OK) return st;

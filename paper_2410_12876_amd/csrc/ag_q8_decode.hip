@@ -865,6 +865,9 @@ hipError_t launch_g(int G, ag_ctx *ctx, hipStream_t s, const dec_args &a) {
 
 }  // namespace
 
+// (and what rounding up to whole ranges adds, at most two workgroups a CU)
+int64_t ag_q8_decode_cost(int64_t units, int max_blocks) { return units * ((int64_t)max_blocks + 1 + kUnitCost) + (1 << 16); }
+
 size_t ag_ws_q8_decode_floats(int num_cu, int G, int D) { return (size_t)4 * num_cu * G * (D + 2); }
 
 hipError_t ag_launch_q8_decode(ag_ctx *ctx, hipStream_t s, const void *q, const void *k_new, const void *v_new, const uint8_t *new_flags,

@@ -47,3 +47,14 @@ def test_flags_and_outputs_of_another_size_or_type_are_refused(lib):  # noqa: F8
     with pytest.raises(ValueError):
         ag.ag_rotate(ctx, q.float(), None, ag.Rope(r.table, r.pos), q, None, stream=0)
     ctx.close()
+
+
+def test_a_page_table_whose_blocks_the_step_cannot_count_is_refused(lib):  # noqa: F811
+    """A step adds up the blocks of all units, and a few more for each, in 32 bits."""
+    B, H, D = 16, 8, 64
+    ctx, c = ag.Context(device=-1, workspace=ag.q8_workspace_bytes(B, 1, H, H, D, 1)), cache(B, H, D, 2, 1)
+    x = torch.zeros(B, H, D, dtype=BF)
+    for blocks, status in ((1 << 24, ag.AG_EUNSUPPORTED), ((1 << 24) - 600, ag.AG_EHIP), (1 << 20, ag.AG_EHIP)):
+        c.c.max_blocks = blocks
+        expect(status, ag.ag_q8_decode_attn, ctx, x, x, x, None, None, 0.1, c, x.clone(), stream=0)
+    ctx.close()
