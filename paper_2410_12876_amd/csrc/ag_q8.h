@@ -108,15 +108,7 @@ __device__ __forceinline__ uint32_t q8_pack2(float lo, float hi) {
 __device__ __forceinline__ float q8_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float q8_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
-// Eight codes (two words) times 2^e as bf16: exact, a code has 4 significant bits.
-__device__ __forceinline__ q8_bf16x8 q8_widen(uint32_t a, uint32_t b, float scale) {
-  const uint4 w = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false)),
-                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true)),
-                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false)),
-                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true))};
-  return __builtin_bit_cast(q8_bf16x8, w);
-}
-// The same as f16 (times a power of two).
+// Eight codes (two words) times a power of two as f16: exact, a code has 4 significant bits.
 __device__ __forceinline__ q8_f16x8 q8_widen16(uint32_t a, uint32_t b, float scale) {
   const uint4 w = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, scale, false)),
                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, scale, true)),

@@ -42,7 +42,7 @@ struct pf_args {
   const ag_q8_meta *meta;
   ag_q8_dev c;
   ag_rope_dev rope;
-  float *part;    // [item][piece][kRows][D + 2]
+  float *part;    // [item][piece][kRows][D + 4]: o, m, l, two of nothing
   int32_t *err;
   int U, Hq, Hkv, L, nw, n_blk, n_qt, n_split;
   float qscale;
