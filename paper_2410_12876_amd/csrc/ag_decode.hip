@@ -516,18 +516,6 @@ struct dec_args {
   ag_ring_dev ring;
 };
 
-// exclusive prefix sum over the wave's lanes (x: the lane's own value); total = the wave's sum
-__device__ __forceinline__ int wave_prefix(int x, int &total) {
-  int y = x;
-  y += __builtin_amdgcn_update_dpp(0, y, 0x111, 0xf, 0xf, false);  // row_shr:1, 2, 4, 8: prefix inside each row of 16
-  y += __builtin_amdgcn_update_dpp(0, y, 0x112, 0xf, 0xf, false);
-  y += __builtin_amdgcn_update_dpp(0, y, 0x114, 0xf, 0xf, false);
-  y += __builtin_amdgcn_update_dpp(0, y, 0x118, 0xf, 0xf, false);
-  y += __builtin_amdgcn_update_dpp(0, y, 0x142, 0xa, 0xf, false);  // row_bcast:15 into rows 1 and 3
-  y += __builtin_amdgcn_update_dpp(0, y, 0x143, 0xc, 0xf, false);  // row_bcast:31 into rows 2 and 3
-  total = __builtin_amdgcn_readlane(y, 63);
-  return y - x;
-}
 
 template <typename T, int D, int G, int NW, bool EVEN>
 __global__ __launch_bounds__(64 * NW, 2) void ag_decode_kernel(dec_args a) {
@@ -592,7 +580,7 @@ __global__ __launch_bounds__(64 * NW, 2) void ag_decode_kernel(dec_args a) {
       if (64 * j < U) {
         int sum_t;
         cnt_t[j] = 64 * j + lane < U ? tiles_of(sl_r[j] & 0x7fffffff) : 0;
-        base_t[j] = total_t + wave_prefix(cnt_t[j], sum_t);
+        base_t[j] = total_t + ag_wave_prefix(cnt_t[j], sum_t);
         total_t += sum_t;
       }
     }
@@ -616,7 +604,7 @@ __global__ __launch_bounds__(64 * NW, 2) void ag_decode_kernel(dec_args a) {
         if (64 * j < U) {
           int sum_i;
           cnt_i[j] = 64 * j + lane < U ? pieces_of(cnt_t[j]) : 0;
-          base_i[j] = total_i + wave_prefix(cnt_i[j], sum_i);
+          base_i[j] = total_i + ag_wave_prefix(cnt_i[j], sum_i);
           total_i += sum_i;
         }
       }
@@ -654,7 +642,7 @@ __global__ __launch_bounds__(64 * NW, 2) void ag_decode_kernel(dec_args a) {
       max_t = max(max_t, t);
     }
     int sum_t;
-    const int pre = wave_prefix(my_t, sum_t);
+    const int pre = ag_wave_prefix(my_t, sum_t);
     for (int o = 32; o > 0; o >>= 1) max_t = max(max_t, __shfl_xor(max_t, o, 64));
     if (lane == 0) { w_sum[wave][0] = sum_t; w_sum[wave][1] = max_t; }
     __syncthreads();

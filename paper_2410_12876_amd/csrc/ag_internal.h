@@ -235,3 +235,18 @@ hipError_t ag_static_scratch(int device, char **ptr);
 // Ring <- the last min(L, n) prompt tokens of every unit (k, v [units, L, D], flags [units, L]).
 hipError_t ag_launch_ring_fill(hipStream_t s, const void *k, const void *v, const uint8_t *flags, int units, int L,
                                int D, ag_dtype dt, int pos0, ag_ring_dev ring);
+
+#ifdef __HIPCC__
+// exclusive prefix sum over the wave's lanes (x: the lane's own value); total = the wave's sum
+__device__ __forceinline__ int ag_wave_prefix(int x, int &total) {
+  int y = x;
+  y += __builtin_amdgcn_update_dpp(0, y, 0x111, 0xf, 0xf, false);  // row_shr:1, 2, 4, 8: prefix inside each row of 16
+  y += __builtin_amdgcn_update_dpp(0, y, 0x112, 0xf, 0xf, false);
+  y += __builtin_amdgcn_update_dpp(0, y, 0x114, 0xf, 0xf, false);
+  y += __builtin_amdgcn_update_dpp(0, y, 0x118, 0xf, 0xf, false);
+  y += __builtin_amdgcn_update_dpp(0, y, 0x142, 0xa, 0xf, false);  // row_bcast:15 into rows 1 and 3
+  y += __builtin_amdgcn_update_dpp(0, y, 0x143, 0xc, 0xf, false);  // row_bcast:31 into rows 2 and 3
+  total = __builtin_amdgcn_readlane(y, 63);
+  return y - x;
+}
+#endif

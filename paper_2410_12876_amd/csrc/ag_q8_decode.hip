@@ -68,17 +68,6 @@ __device__ __forceinline__ float2 get_pair(const float *p) {
   const uint64_t x = __hip_atomic_load(reinterpret_cast<const uint64_t *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
   return make_float2(__uint_as_float((uint32_t)x), __uint_as_float((uint32_t)(x >> 32)));
 }
-__device__ __forceinline__ int wave_prefix(int x, int &total) {
-  int y = x;
-  y += __builtin_amdgcn_update_dpp(0, y, 0x111, 0xf, 0xf, false);
-  y += __builtin_amdgcn_update_dpp(0, y, 0x112, 0xf, 0xf, false);
-  y += __builtin_amdgcn_update_dpp(0, y, 0x114, 0xf, 0xf, false);
-  y += __builtin_amdgcn_update_dpp(0, y, 0x118, 0xf, 0xf, false);
-  y += __builtin_amdgcn_update_dpp(0, y, 0x142, 0xa, 0xf, false);
-  y += __builtin_amdgcn_update_dpp(0, y, 0x143, 0xc, 0xf, false);
-  total = __builtin_amdgcn_readlane(y, 63);
-  return y - x;
-}
 // Over the wave's lanes (register exchanges: no addresses that live in registers, as lane shuffles have them)
 __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
   auto dpp = [](uint32_t y, auto ctrl) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)y, decltype(ctrl)::value, 0xf, 0xf, false); };
@@ -550,7 +539,7 @@ __global__ __launch_bounds__(64 * NW, 2) void ag_q8_decode_kernel(dec_args a) {
     for (int j = 0; j < 2; ++j) {
       if (64 * j + lane < U) t[j] = items_of(sl_r[j]);
       cost[j] = t[j] ? t[j] + kUnitCost : 0;
-      pre_t[j] = total + wave_prefix(cost[j], sum);
+      pre_t[j] = total + ag_wave_prefix(cost[j], sum);
       total += sum;
     }
     items = total - U * kUnitCost;
@@ -563,7 +552,7 @@ __global__ __launch_bounds__(64 * NW, 2) void ag_q8_decode_kernel(dec_args a) {
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         p[j] = t[j] ? pieces_of(t[j]) : 0;
-        pre_p[j] = pieces + wave_prefix(p[j], sum);
+        pre_p[j] = pieces + ag_wave_prefix(p[j], sum);
         pieces += sum;
       }
       if (pieces <= grid || last || U >= grid) break;
@@ -592,7 +581,7 @@ __global__ __launch_bounds__(64 * NW, 2) void ag_q8_decode_kernel(dec_args a) {
       my_t += items_of(n) + kUnitCost;
       max_t = max(max_t, items_of(n));
     }
-    int pre_t = wave_prefix(my_t, sum);
+    int pre_t = ag_wave_prefix(my_t, sum);
     max_t = (int)wave_max((uint32_t)max_t);
     if (lane == 0) { w_sum[wave][0] = sum; w_sum[wave][1] = max_t; }
     __syncthreads();

@@ -41,18 +41,6 @@ struct fill_args {
   int Hkv, L, nw, n_blk;
 };
 
-// Sum over the lanes before this one; total: the wave's sum.
-__device__ __forceinline__ int wave_prefix(int x, int &total) {
-  int y = x;
-  y += __builtin_amdgcn_update_dpp(0, y, 0x111, 0xf, 0xf, false);
-  y += __builtin_amdgcn_update_dpp(0, y, 0x112, 0xf, 0xf, false);
-  y += __builtin_amdgcn_update_dpp(0, y, 0x114, 0xf, 0xf, false);
-  y += __builtin_amdgcn_update_dpp(0, y, 0x118, 0xf, 0xf, false);
-  y += __builtin_amdgcn_update_dpp(0, y, 0x142, 0xa, 0xf, false);
-  y += __builtin_amdgcn_update_dpp(0, y, 0x143, 0xc, 0xf, false);
-  total = __builtin_amdgcn_readlane(y, 63);
-  return y - x;
-}
 // The flags of 16 tokens from t on as bits (those past L: 0).  A row of flags starts at any address.
 __device__ __forceinline__ uint32_t flag_bits(const uint8_t *f, int t, int L) {
   uint32_t bits = 0;
@@ -136,7 +124,7 @@ __global__ __launch_bounds__(4 * D, 4) void ag_q8_fill_kernel(fill_args a) {
   const int32_t *off = nullptr;
   if constexpr (CHUNKS > 0) {
     int sum;
-    before = wave_prefix(mine, sum);
+    before = ag_wave_prefix(mine, sum);
     if (lane == 0) s_sum[wave] = sum;
     __syncthreads();
     kept = 0;
