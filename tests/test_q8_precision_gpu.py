@@ -179,3 +179,20 @@ def test_many_small_weights_are_not_lost(rows, bits):
     e = row_errors(out, (value.double() + w * low + w_own * v.double().repeat_interleave(G, dim=1)) / (1 + w + w_own))
     print("turn", rows, bits, "row errors: mean %.2e, worst %.2e" % (e.mean().item(), e.max().item()), flush=True)
     assert e.max() <= bar()
+
+
+# ------------------------------------------------------------------------------------------------------------------ large scores
+@pytest.mark.parametrize("Hq,H,D,lens,kind", [(4, 2, 128, [0, 700], "runs"), (8, 2, 64, [130, 64], "rand"), (2, 2, 128, [1500, 90], "none")])
+def test_turns_at_large_scores(Hq, H, D, lens, kind):
+    g, L, spread = gen(sum(lens) + D), 260, 7.0
+    ref = cache_of(1, H, D, lens, L, g)
+    q, k, v, f = some(g, 1, Hq, L, D), some(g, 1, H, L, D), some(g, 1, H, L, D), flags_of(g, kind, 1, H, L)
+    assert turn_error(ref, g, q, k, v, f, spread * D ** -0.5, 1).max() <= bar(spread)
+
+
+@pytest.mark.parametrize("B,H,G,D,longest", [(1, 8, 4, 128, 3000), (130, 10, 1, 64, 320), (65, 4, 2, 64, 900)])
+def test_steps_at_large_scores(B, H, G, D, longest):
+    g, spread = gen(D + longest + 1), 7.0
+    ref = many_units(B, H, D, longest, g)
+    q, k, v, f = some(g, B, H * G, D), some(g, B, H, D), some(g, B, H, D), flags_of(g, "rand", B, H, 1)[:, :, 0].contiguous()
+    assert step_error(ref, g, q, k, v, f, spread * D ** -0.5, 1).max() <= bar(spread)
