@@ -9,13 +9,16 @@
 //     f16 (exact, two values an instruction), into S^T = K q^T and O^T = V^T p^T on v_mfma_f32_16x16x32_f16: no LDS, no barrier.  A wave has
 //     two pages in flight, 16 to 32 KiB; a piece's registers are asked for again as soon as it is used up.
 //   * Queries are f16 times a power of two per row, weights are f16 relative to a reference that is moved only when their sum passes 2^15:
-//     11 bits of each, as the codes have 4.  (A weight in three bf16 parts in the columns that G < 16 leaves idle was as exact and slower:
-//     32 sequences of 32 heads 533 us a 4 steps, now 440.)
+//     11 bits of each, as the codes have 4; row sums add up the rounded weights.  The reference lies 2^-8 below the largest of the page that set it,
+//     so weights down to 2^-33 of that count; in the wave that has the tail the tail sets it, and those down to 2^-21 do.  (A weight in three
+//     bf16 parts in the columns that G < 16 leaves idle kept 24 bits: 32 sequences of 32 heads 533 us a 4 steps, now 443; output rows are off by 1.7e-3 of
+//     their size either way, which the store's rounding gives.)
 //   * The workgroup turns its queries and the new key together, into LDS: a lane's own row by itself took 64 lines a load.  The barrier
 //     after it waits for LDS alone, and the pages are asked for behind it: ahead of it they held up the small loads.
 //   * The tail is a page in bf16; the new token's row is put into it in registers, so that it is one row more.  The wave that has it also
-//     stores that row, or, if it is the block's last, the whole block in 8 bits.
-//   * 32 sequences of 32 heads over 400 to 4096 rows: 109 us a step, 5.2 TB/s of pages; a chat of 8 heads and hundreds of rows: 10 us, of
+//     stores that row, or, if it is the block's last, the whole block in 8 bits.  Its own score takes what rounding its key to bf16 leaves over
+//     as one more product: without, scores of 7 times the usual spread put rows off by 2e-2 of their size, now by 4.6e-3.
+//   * 32 sequences of 32 heads over 400 to 4096 rows: 111 us a step, 5.1 TB/s of pages; a chat of 8 heads and hundreds of rows: 10 us, of
 //     which the launch and about six dependent round trips are all.
 //   * Segments: if the whole step gives every workgroup at most one piece of a unit (a few rounds of its waves), those; if there are more
 //     units than workgroups and all are short, one, two or four waves a unit; else all items end to end, in equal ranges.

@@ -3,7 +3,8 @@
 // For new token j of a unit the visible rows are: all rows that the cache held, the call's own kept tokens before j, and j itself.
 // ag_q8_fill_kernel (launched first) leaves the tail's rows and the kept tokens, turned and packed, as tiles of 64 rows in f16;
 // the full blocks of the cache are read as they are.  So the keys of a unit are one sequence of tiles -- its pages, then those --
-// of which row j sees the first `bound_j` rows; an evicted token's own key and value, which are in none of them, are what its state starts from.
+// of which row j sees the first `bound_j` rows; an evicted token's own key and value, which are in none of them, are what its state starts from
+// (and a kept one's that sees nothing else).
 //   * A workgroup of 4 waves owns 128 query rows of a unit (token by token, the group's heads of a token side by side) and every wave 32 of
 //     them, with a lane owning one column: S^T = K q^T, O^T = V^T p^T on v_mfma_f32_32x32x16_f16, P passes from the first product's
 //     accumulators into the second one's operand without leaving the lane.
@@ -14,11 +15,15 @@
 //     product before it: 765 us in place of 900 for 4096 tokens of 8 heads in 2 groups over 13000 rows, with the pages' numbers and scales
 //     looked up 64 tiles at a time (tile by tile they were waited for in every step).  Forming one half's weights between the other half's
 //     products, which the compiler can be made to do, gained nothing over this: the second workgroup of the CU fills those gaps already.
-//   * Both products are in f16, whose 11 bits keep scores and weights to 2^-12 of themselves (in bf16, 2^-9: an output row's error grew from 1.7e-3
-//     to 2.9e-3 of its size, and with scores of 7 times the usual spread a weight was off by a hundredth).  Its narrow range is why queries and
-//     tiles carry exponents; tiles of too different values are taken row by row on the vector ALU.
+//   * Both products are in f16, whose 11 bits keep operands to 2^-12 of themselves (in bf16, 2^-9: an output row's error grew from 1.7e-3
+//     to 2.9e-3 of its size, and with scores of 7 times the usual spread a weight was off by a hundredth).  Its narrow range is why queries,
+//     tiles and a token's own value carry exponents; tiles of too different values are taken row by row on the vector ALU.
+//   * Weights are f16 too, relative to a reference that lies 2^-8 below the largest (score plus exponent) of the tile that set it: down to
+//     2^-22 of that they keep 11 bits, down to 2^-33 some.  The row sum adds up the rounded ones, so their rounding cancels where many are
+//     alike.  (Against the largest itself and with the unrounded sum, 300000 rows at 2^-25.5 of it put a row off by 1.5e-2 of its size, now by 2.4e-3,
+//     which the store's rounding gives.)
 //   * No maximum is taken in the common case: weights are formed against the reference as it stands, and only if their sum passes 2^15 is
-//     it moved.
+//     it moved.  The first tile always sets it.
 //   * Few items and long caches: the tiles of an item are cut into up to n_split pieces, whose states a second kernel adds up.
 #include <algorithm>
 
