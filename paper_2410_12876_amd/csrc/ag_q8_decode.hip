@@ -39,7 +39,7 @@ constexpr int kFewUnits = 128;
 constexpr int kWholeRounds = 2;
 constexpr int kValueBits = 9;     // a page's values in f16 are below 1 (exact: a code has 4 bits, the least is 2^-9), as the tail's are of unit size
 // Bits by which a page's reference may lie below the one that a tail has left: its weights are then 2^-4 at most, and those down to 2^-21 of
-// the largest count.  (Values of unit size: 5.  Coming down costs a step of few rows 0.4 us of 9.6.)
+// the largest count.  (Values of unit size: 5.  Coming down costs a step of few rows 0.5 us of 9.7.)
 constexpr float kHighBits = kQ8TopBits + 4;
 constexpr int kArriveSplit = 64;  // workgroups from which their arrivals are counted at several addresses
 // What a unit costs a workgroup beside its items, in items, where all units are cut into equal ranges: the start of a segment, the tail's two
@@ -161,26 +161,12 @@ template <int D, int G> struct wave_q8 {
 
   // How far the reference may come down: the state grows by as much, and must not overflow (what is not finite already stays so).
   __device__ __forceinline__ float lower() const {
-    float top[4];  // (the larger of three magnitudes an instruction; four chains, or every one would wait for the one before it)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      top[r] = fabsf(o[0][r]);
-#pragma unroll
-      for (int f = 1; f < VF; f += 2) {
-        const float x = o[f][r], y = o[f + 1 < VF ? f + 1 : f][r];
-        asm("v_max3_f32 %0, %0, |%1|, |%2|" : "+v"(top[r]) : "v"(x), "v"(y));
-      }
-    }
-    if (!__any(!(top[0] < 0x1p59f) | !(top[1] < 0x1p59f) | !(top[2] < 0x1p59f) | !(top[3] < 0x1p59f))) return -(float)kQ8TileMinExp;
-    uint32_t most = 0;
+    float top = 0.f;
 #pragma unroll
     for (int f = 0; f < VF; ++f)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const uint32_t x = __float_as_uint(o[f][r]) & 0x7fffffffu;
-        most = max(most, x < 0x7f800000u ? x : 0u);
-      }
-    return (float)max(0, min(-kQ8TileMinExp, 127 + 120 - (int)(wave_max(most) >> 23)));
+      for (int r = 0; r < 4; ++r) top = fmaxf(top, fabsf(o[f][r]) < INFINITY ? fabsf(o[f][r]) : 0.f);
+    return (float)max(0, min(-kQ8TileMinExp, 127 + 120 - (int)(wave_max(__float_as_uint(top)) >> 23)));
   }
 
   // A wave's pages: lane x holds the number and the exponents of its page x (of at most 64 at a time); two pages are in flight.
