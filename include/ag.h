@@ -90,7 +90,8 @@ const char *ag_last_error(const ag_ctx *ctx);
 size_t ag_workspace_bytes(int B, int L, int Hq, int Hkv, int D, ag_dtype dtype, int d_in, int64_t cache_rows);
 
 /* Synchronise `stream`, read and clear the sticky device error word.  AG_OK, AG_ECAPACITY, or AG_EINVAL (a position outside
- * the table of an ag_rope); where both have happened, one call reports AG_ECAPACITY and the next one AG_EINVAL.
+ * the table of an ag_rope, a node of a tree that names none before it); where several have happened, one call reports one of them,
+ * AG_ECAPACITY first.
  * (Kernel timing and machine probes for benchmarks are declared in ag_bench.h; they are no part of the method.) */
 ag_status ag_poll_error(ag_ctx *ctx, void *hip_stream);
 
@@ -304,6 +305,16 @@ ag_status ag_rotate(ag_ctx *ctx, void *hip_stream, const void *q, const void *k,
                     int D, const ag_rope *rope, void *q_out, void *k_out);
 
 /*
+ * Queries and keys normalised head by head and then turned by their positions, in one launch: every vector x of D values of q (k) becomes
+ *   n_i = (x_i r) w_i,   r = 1 / sqrt(mean_i x_i^2 + eps),   w = q_weight (k_weight)
+ * and n is turned as ag_rotate turns it; all in 32 bits, products and sums rounded one by one, one rounding to `dtype` at the end.  rope = NULL: n
+ * itself.  q_weight, k_weight [D] in `dtype`; eps >= 2^-100; k, k_out and k_weight may be NULL together (Hkv is then ignored).  Layouts, types,
+ * D and alignment (the weights' too) as for ag_rotate; q_out may be q, k_out may be k.  Needs no workspace.
+ */
+ag_status ag_norm_rotate(ag_ctx *ctx, void *hip_stream, const void *q, const void *k, ag_dtype dtype, int B, int Hq, int Hkv, int L,
+                         int D, const void *q_weight, const void *k_weight, float eps, const ag_rope *rope, void *q_out, void *k_out);
+
+/*
  * Paged 8-bit cache.  Unit u = b * Hkv + g counts its rows in order of arrival; rows 64 j .. 64 j + 63 are its block j.
  *   - A full block is held in 8 bits: value = code 2^e, the codes e4m3 numbers (round to nearest even), e the least integer >= -100
  *     with max |x| 2^-e <= 448 over the block's finite values, for K and V each; what is not finite becomes NaN.  Its codes lie in page
@@ -358,6 +369,66 @@ ag_status ag_q8_prefill_attn(ag_ctx *ctx, void *hip_stream, const void *q, const
  */
 ag_status ag_q8_decode_attn(ag_ctx *ctx, void *hip_stream, const void *q, const void *k_new, const void *v_new,
                             const uint8_t *new_flags, int Hq, const ag_rope *rope, float scale, ag_q8_cache *cache, void *out);
+
+/*
+ * Trees of drafted tokens over the paged 8-bit cache (several continuations of a sequence, verified at once).  Every sequence has L nodes,
+ * L <= AG_Q8_TREE_MOST; parent [B, L] (device int32) names the node that a node continues, parent[b][t] < t, negative: none (it continues the
+ * cache).  A parent that is not before its node counts as none (ag_poll_error: AG_EINVAL).  Positions (rope->pos) are the caller's:
+ * nodes of one depth share theirs.
+ *
+ * ag_q8_tree_attn: node t of query head i (KV head g = i / (Hq/Hkv)) sees the unit's rows as the cache holds them, those nodes above it
+ * in its tree with flags[b,g,.] != 0 (flags = NULL: all), and itself; out as in ag_q8_prefill_attn, of which a chain is the case
+ * parent[t] = t - 1.  The cache is only read.  q, out [B, Hq, L, D]; k, v [B, Hkv, L, D].  One launch.
+ * B * Hkv * (max_blocks + 16) times the number of 128-row tiles of L * (Hq / Hkv) rows must stay below 2^31 - 2^16.
+ *
+ * ag_q8_tree_append: the accepted path joins the cache: of the nodes above last[b] (device int32 [B]; negative: none) and last[b] itself, those
+ * with flags[b,g,.] != 0, in order, as ag_q8_append appends them.  A last[b] >= L counts as none (ag_poll_error: AG_EINVAL).  Needs no workspace.
+ */
+#define AG_Q8_TREE_MOST 256
+
+/* Workspace that covers ag_q8_tree_attn with up to L nodes on caches of up to max_blocks. */
+size_t ag_q8_tree_workspace_bytes(int B, int L, int Hq, int Hkv, int D, int max_blocks);
+
+ag_status ag_q8_tree_attn(ag_ctx *ctx, void *hip_stream, const void *q, const void *k, const void *v, const uint8_t *flags,
+                          const int32_t *parent, int L, int Hq, const ag_rope *rope, float scale, const ag_q8_cache *cache, void *out);
+
+ag_status ag_q8_tree_append(ag_ctx *ctx, void *hip_stream, const void *k, const void *v, const uint8_t *flags, const int32_t *parent,
+                            const int32_t *last, int L, const ag_rope *rope, ag_q8_cache *cache);
+
+/*
+ * A pool of pages that several caches share (beams, sequences with a common beginning).  ref (device int32 [n_pages]) counts for every page the
+ * entries of all tables that name it; 0: the page is free.  A program starts with ref = 0 and tables of -1 and leaves both to these calls,
+ * which write cache->page (entries outside [0, n_pages) name no page).  At most 2^25 pages.
+ *
+ * ag_q8_reserve: every unit gets pages for the blocks that `rows` more rows would fill, as far as they have none: blocks len / 64 up to
+ * (len + rows) / 64 - 1.  The free pages are handed out in increasing order, to units and blocks in increasing order.  Where pages or blocks of
+ * the table run out, the entries stay without one (ag_poll_error: AG_ECAPACITY).
+ *
+ * ag_q8_fork: sequence b of dst becomes what sequence parent[b] (device int32 [dst->B]) of src is: its length, a copy of its tails, and its full
+ * blocks, shared; later blocks have no page (ag_q8_reserve).  A parent outside [0, src->B): the sequence becomes empty.  What dst's table named
+ * before is given back, what it names now is counted; src stays as it is (ag_q8_release gives it back).  src and dst are different caches over
+ * one pool: the same k, v, scales, n_pages, Hkv and D, other tails, tables and lengths, dst->max_blocks >= src->max_blocks.  One launch.
+ *
+ * ag_q8_release: the sequences with which[b] != 0 (device uint8 [B]; NULL: all) give back all their pages and become empty.
+ *
+ * ag_q8_compact_pages: the pages in use move together: used[0] (device int32) receives their number N, and the i-th page in use of those
+ * behind N (in increasing order) moves, with its scales and count, to the i-th free one of those before.  moved (device int32 [n_pages]) receives
+ * every page's new number, -1 for free ones.  Of cache only k, v, scales and n_pages count.  Then every cache over the pool needs
+ * ag_q8_remap: its table's entries become moved[entry].  Pages that are free afterwards hold anything.
+ *
+ * ag_q8_pool_workspace_bytes covers all of these on caches of up to B * Hkv units; only ag_q8_reserve and ag_q8_compact_pages need any.
+ */
+size_t ag_q8_pool_workspace_bytes(int B, int Hkv, int n_pages);
+
+ag_status ag_q8_reserve(ag_ctx *ctx, void *hip_stream, ag_q8_cache *cache, int32_t *ref, int rows);
+
+ag_status ag_q8_fork(ag_ctx *ctx, void *hip_stream, const ag_q8_cache *src, const int32_t *parent, ag_q8_cache *dst, int32_t *ref);
+
+ag_status ag_q8_release(ag_ctx *ctx, void *hip_stream, ag_q8_cache *cache, int32_t *ref, const uint8_t *which);
+
+ag_status ag_q8_compact_pages(ag_ctx *ctx, void *hip_stream, ag_q8_cache *cache, int32_t *ref, int32_t *moved, int32_t *used);
+
+ag_status ag_q8_remap(ag_ctx *ctx, void *hip_stream, ag_q8_cache *cache, const int32_t *moved);
 
 #ifdef __cplusplus
 }

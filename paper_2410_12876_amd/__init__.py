@@ -28,7 +28,9 @@ EXPORTS = ["ag_create", "ag_destroy", "ag_last_error", "ag_workspace_bytes", "ag
            "ag_timing_kernels", "ag_timing_kernel_name", "ag_timing_enable", "ag_timing_read",
            "ag_probe_mfma", "ag_probe_mfma_data", "ag_probe_mfma_duty", "ag_probe_copy", "ag_probe_projection_tile", "ag_gate", "ag_rmsnorm_gate", "ag_compact_kv", "ag_pack_row_off", "ag_prefill_attn", "ag_prefill_attn_recent",
            "ag_compact_prefill_attn", "ag_project_compact_kv", "ag_project_compact_workspace_bytes", "ag_decode_attn", "ag_decode_attn_static", "ag_decode_static_scratch_bytes", "ag_decode_scratch_bytes", "ag_recent_fill", "ag_decode_attn_recent", "ag_gate_mha", "ag_gate_mha_workspace_bytes",
-           "ag_rotate", "ag_q8_workspace_bytes", "ag_q8_append", "ag_q8_prefill_attn", "ag_q8_decode_attn"]
+           "ag_rotate", "ag_q8_workspace_bytes", "ag_q8_append", "ag_q8_prefill_attn", "ag_q8_decode_attn",
+           "ag_norm_rotate", "ag_q8_tree_workspace_bytes", "ag_q8_tree_attn", "ag_q8_tree_append", "ag_q8_pool_workspace_bytes", "ag_q8_reserve",
+           "ag_q8_fork", "ag_q8_release", "ag_q8_compact_pages", "ag_q8_remap"]
 
 
 class ag_recent_ring(C.Structure):
@@ -147,6 +149,26 @@ def load() -> C.CDLL:
     lib.ag_q8_prefill_attn.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, C.POINTER(ag_rope), f32, C.POINTER(ag_q8_cache), vp]
     lib.ag_q8_decode_attn.restype = C.c_int
     lib.ag_q8_decode_attn.argtypes = [vp, vp, vp, vp, vp, vp, i32, C.POINTER(ag_rope), f32, C.POINTER(ag_q8_cache), vp]
+    lib.ag_norm_rotate.restype = C.c_int
+    lib.ag_norm_rotate.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp, vp, f32, C.POINTER(ag_rope), vp, vp]
+    lib.ag_q8_tree_workspace_bytes.restype = C.c_size_t
+    lib.ag_q8_tree_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32]
+    lib.ag_q8_tree_attn.restype = C.c_int
+    lib.ag_q8_tree_attn.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i32, C.POINTER(ag_rope), f32, C.POINTER(ag_q8_cache), vp]
+    lib.ag_q8_tree_append.restype = C.c_int
+    lib.ag_q8_tree_append.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, C.POINTER(ag_rope), C.POINTER(ag_q8_cache)]
+    lib.ag_q8_pool_workspace_bytes.restype = C.c_size_t
+    lib.ag_q8_pool_workspace_bytes.argtypes = [i32, i32, i32]
+    lib.ag_q8_reserve.restype = C.c_int
+    lib.ag_q8_reserve.argtypes = [vp, vp, C.POINTER(ag_q8_cache), vp, i32]
+    lib.ag_q8_fork.restype = C.c_int
+    lib.ag_q8_fork.argtypes = [vp, vp, C.POINTER(ag_q8_cache), vp, C.POINTER(ag_q8_cache), vp]
+    lib.ag_q8_release.restype = C.c_int
+    lib.ag_q8_release.argtypes = [vp, vp, C.POINTER(ag_q8_cache), vp, vp]
+    lib.ag_q8_compact_pages.restype = C.c_int
+    lib.ag_q8_compact_pages.argtypes = [vp, vp, C.POINTER(ag_q8_cache), vp, vp, vp]
+    lib.ag_q8_remap.restype = C.c_int
+    lib.ag_q8_remap.argtypes = [vp, vp, C.POINTER(ag_q8_cache), vp]
     import torch  # noqa: F401  (the binding module uses its libraries)
     from . import _binding
     _lib, _native = lib, _binding
@@ -443,3 +465,57 @@ def ag_q8_decode_attn(ctx: Context, q, k_new, v_new, new_flags, rope: Optional[R
     """q, out [B, Hq, D]; k_new, v_new [B, Hkv, D]; new_flags u8 [B, Hkv] or None; rope.pos [n_axes, B, 1]; cache updated in place."""
     ctx._check(ctx._native.q8_decode_attn(ctx._addr, stream, q, k_new, v_new, new_flags, rope._of(cache.D, cache.B, 1) if rope is not None else None,
                                           scale, cache.c, out))
+
+
+def ag_norm_rotate(ctx: Context, q, k, q_weight, k_weight, eps: float, rope: Optional[Rope], q_out, k_out, stream=None) -> None:
+    """q, q_out [B, Hq, L, D], k, k_out [B, Hkv, L, D] (or None), q_weight, k_weight [D]: every head's vector normalised by its root mean
+    square and turned by rope.pos [n_axes, B, L] (None: not turned); q_out may be q, k_out may be k."""
+    ctx._check(ctx._native.norm_rotate(ctx._addr, stream, q, k, q_weight, k_weight, eps,
+                                       rope._of(q.shape[-1], q.shape[0], q.shape[2]) if rope is not None else None, q_out, k_out))
+
+
+def q8_tree_workspace_bytes(B: int, L: int, Hq: int, Hkv: int, D: int, max_blocks: int) -> int:
+    return int(load().ag_q8_tree_workspace_bytes(B, L, Hq, Hkv, D, max_blocks))
+
+
+def ag_q8_tree_attn(ctx: Context, q, k, v, flags, parent, rope: Optional[Rope], scale: float, cache: Q8Cache, out, stream=None) -> None:
+    """q, out [B, Hq, L, D]; k, v [B, Hkv, L, D]; flags u8 [B, Hkv, L] or None; parent i32 [B, L] (-1: none): attention of every node of a tree of
+    drafted tokens over the cache, its kept ancestors and itself.  The cache is only read."""
+    ctx._check(ctx._native.q8_tree_attn(ctx._addr, stream, q, k, v, flags, parent,
+                                        rope._of(cache.D, cache.B, q.shape[2]) if rope is not None else None, scale, cache.c, out))
+
+
+def ag_q8_tree_append(ctx: Context, k, v, flags, parent, last, rope: Optional[Rope], cache: Q8Cache, stream=None) -> None:
+    """k, v, flags, parent as for ag_q8_tree_attn; last i32 [B] (-1: none): the kept nodes from the root to last join the cache."""
+    ctx._check(ctx._native.q8_tree_append(ctx._addr, stream, k, v, flags, parent, last,
+                                          rope._of(cache.D, cache.B, k.shape[2]) if rope is not None else None, cache.c))
+
+
+def q8_pool_workspace_bytes(B: int, Hkv: int, n_pages: int) -> int:
+    return int(load().ag_q8_pool_workspace_bytes(B, Hkv, n_pages))
+
+
+def ag_q8_reserve(ctx: Context, cache: Q8Cache, ref, rows: int, stream=None) -> None:
+    """ref i32 [n_pages] (table entries that name each page): every unit gets pages for `rows` more rows (cache.page, ref written)."""
+    ctx._check(ctx._native.q8_reserve(ctx._addr, stream, cache.c, ref, rows))
+
+
+def ag_q8_fork(ctx: Context, src: Q8Cache, parent, dst: Q8Cache, ref, stream=None) -> None:
+    """parent i32 [dst.B]: sequence b of dst becomes what sequence parent[b] of src is (-1: empty), full blocks shared; ref counts them."""
+    ctx._check(ctx._native.q8_fork(ctx._addr, stream, src.c, parent, dst.c, ref))
+
+
+def ag_q8_release(ctx: Context, cache: Q8Cache, ref, which=None, stream=None) -> None:
+    """which u8 [B] or None (all): those sequences give back their pages and become empty."""
+    ctx._check(ctx._native.q8_release(ctx._addr, stream, cache.c, ref, which))
+
+
+def ag_q8_compact_pages(ctx: Context, cache: Q8Cache, ref, moved, used, stream=None) -> None:
+    """The pages in use move to the front of the pool: moved i32 [n_pages] receives their new numbers, used i32 [1] how many there are.  Then
+    ag_q8_remap on every cache over the pool."""
+    ctx._check(ctx._native.q8_compact_pages(ctx._addr, stream, cache.c, ref, moved, used))
+
+
+def ag_q8_remap(ctx: Context, cache: Q8Cache, moved, stream=None) -> None:
+    """The table's entries become moved[entry]."""
+    ctx._check(ctx._native.q8_remap(ctx._addr, stream, cache.c, moved))

@@ -109,7 +109,7 @@ void ag_destroy(ag_ctx *ctx) {
 static const char *const kKernelNames[AG_K_COUNT] = {"gate", "gate_finalize", "flag_scan", "compact",
                                                      "prefill", "decode_partial", "decode_merge",
                                                      "mha_proj", "mha_attn", "norm_gate", "rotate", "q8_fill",
-                                                     "q8_prefill", "q8_decode"};
+                                                     "q8_prefill", "q8_decode", "norm_rotate", "q8_tree", "q8_fork", "q8_pages"};
 
 int ag_timing_kernels(void) { return AG_K_COUNT; }
 
@@ -196,11 +196,12 @@ ag_status ag_poll_error(ag_ctx *ctx, void *hip_stream) {
   AG_HIP(hipMemcpyAsync(&h, ctx->d_err, sizeof(h), hipMemcpyDeviceToHost, (hipStream_t)hip_stream));
   AG_HIP(hipStreamSynchronize((hipStream_t)hip_stream));
   if (h) {
-    const int32_t left = h & 1 ? h & ~1 : 0;  // one error a call
+    const int32_t left = h & (h - 1);  // one error a call, the lowest bit first
     AG_HIP(hipMemsetD32Async((hipDeviceptr_t)ctx->d_err, left, 1, (hipStream_t)hip_stream));
     AG_HIP(hipStreamSynchronize((hipStream_t)hip_stream));
     if (h & 1) return ag_fail(ctx, AG_ECAPACITY, "a cache unit overflowed its capacity; the extra rows were dropped");
-    return ag_fail(ctx, AG_EINVAL, "a position lies outside the rotation table; the nearest row was used");
+    if (h & 2) return ag_fail(ctx, AG_EINVAL, "a position lies outside the rotation table; the nearest row was used");
+    return ag_fail(ctx, AG_EINVAL, "a tree's node names a parent that is not before it, or an accepted node that is not there; it counts as none");
   }
   return AG_OK;
 }

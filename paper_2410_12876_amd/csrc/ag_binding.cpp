@@ -340,11 +340,122 @@ AG_BINDING(q8_decode_attn, 8) {
   return call([&] { return ag_q8_decode_attn(ctx, s, qp, kp, v, f, Hq, r, scale, c, out); });
 }
 
+// int32 numbers, n of them.
+int32_t *ints_of(PyObject *o, int64_t n, const char *msg) {
+  const at::Tensor &t = tensor(o);
+  if (t.scalar_type() != at::kInt || t.numel() != n) fail(PyExc_ValueError, msg);
+  return ptr_as<int32_t>(o);
+}
+
+// q, k, q_weight, k_weight, eps, rope, q_out, k_out
+AG_BINDING(norm_rotate, 8) {
+  const at::Tensor &q = tensor(a[0]);
+  const int B = dim(q, 4, 0), Hq = dim(q, 4, 1), L = dim(q, 4, 2), D = dim(q, 4, 3);
+  int Hkv = 0;
+  if (a[1] != Py_None) {
+    const at::Tensor &k = tensor(a[1]);
+    Hkv = dim(k, 4, 1);
+    if (k.scalar_type() != q.scalar_type() || k.size(0) != B || k.size(2) != L || k.size(3) != D)
+      fail(PyExc_ValueError, "norm_rotate: q and k differ in more than their heads");
+    if (THPVariable_Check(a[7])) like(tensor(a[7]), k, "norm_rotate: k_out and k differ");
+  }
+  for (int i = 2; i < 4; ++i)
+    if (THPVariable_Check(a[i]) && (tensor(a[i]).scalar_type() != q.scalar_type() || tensor(a[i]).numel() != D))
+      fail(PyExc_ValueError, "norm_rotate: a weight is not one value of the vectors' type for each of theirs");
+  if (THPVariable_Check(a[6])) like(tensor(a[6]), q, "norm_rotate: q_out and q differ");
+  const ag_dtype dt = dtype_of(q);
+  const void *qp = ptr(a[0]), *k = ptr(a[1]), *qw = ptr(a[2]), *kw = ptr(a[3]);
+  const float eps = float_of(a[4]);
+  const ag_rope *r = struct_of<ag_rope>(a[5]);
+  void *qo = ptr(a[6]), *ko = ptr(a[7]);
+  return call([&] { return ag_norm_rotate(ctx, s, qp, k, dt, B, Hq, Hkv, L, D, qw, kw, eps, r, qo, ko); });
+}
+
+// q, k, v, flags, parent, rope, scale, cache, out
+AG_BINDING(q8_tree_attn, 9) {
+  const at::Tensor &q = tensor(a[0]), &k = tensor(a[1]);
+  const int Hq = dim(q, 4, 1), L = dim(q, 4, 2);
+  const ag_rope *r = struct_of<ag_rope>(a[5]);
+  const float scale = float_of(a[6]);
+  const ag_q8_cache *c = struct_of<ag_q8_cache>(a[7]);
+  like_cache(k, c, 4);
+  like(tensor(a[2]), k, "k and v differ");
+  like(tensor(a[8]), q, "out and q differ");
+  if (q.scalar_type() != k.scalar_type() || q.size(0) != k.size(0) || k.size(2) != L || q.size(3) != k.size(3))
+    fail(PyExc_ValueError, "q and k differ in more than their heads");
+  const void *qp = ptr(a[0]), *kp = ptr(a[1]), *v = ptr(a[2]);
+  const uint8_t *f = flags_of(a[3], k.size(0) * k.size(1) * L);
+  const int32_t *parent = ints_of(a[4], k.size(0) * L, "parent is not an int32 number for every node");
+  void *out = ptr(a[8]);
+  return call([&] { return ag_q8_tree_attn(ctx, s, qp, kp, v, f, parent, L, Hq, r, scale, c, out); });
+}
+
+// k, v, flags, parent, last, rope, cache
+AG_BINDING(q8_tree_append, 7) {
+  const at::Tensor &k = tensor(a[0]);
+  const int L = dim(k, 4, 2);
+  const ag_rope *r = struct_of<ag_rope>(a[5]);
+  ag_q8_cache *c = struct_of<ag_q8_cache>(a[6]);
+  like_cache(k, c, 4);
+  like(tensor(a[1]), k, "k and v differ");
+  const void *kp = ptr(a[0]), *v = ptr(a[1]);
+  const uint8_t *f = flags_of(a[2], k.size(0) * k.size(1) * L);
+  const int32_t *parent = ints_of(a[3], k.size(0) * L, "parent is not an int32 number for every node");
+  const int32_t *last = ints_of(a[4], k.size(0), "last is not an int32 number for every sequence");
+  return call([&] { return ag_q8_tree_append(ctx, s, kp, v, f, parent, last, L, r, c); });
+}
+
+int32_t *ref_of(PyObject *o, const ag_q8_cache *c) { return ints_of(o, c ? c->n_pages : 0, "not an int32 number for every page"); }
+
+// cache, ref, rows
+AG_BINDING(q8_reserve, 3) {
+  ag_q8_cache *c = struct_of<ag_q8_cache>(a[0]);
+  int32_t *ref = ref_of(a[1], c);
+  const int64_t rows = int64_of(a[2]);
+  if (rows > 0x7fffffff) fail(PyExc_ValueError, "rows does not fit");
+  return call([&] { return ag_q8_reserve(ctx, s, c, ref, rows < 0 ? -1 : (int)rows); });
+}
+
+// src, parent, dst, ref
+AG_BINDING(q8_fork, 4) {
+  const ag_q8_cache *from = struct_of<ag_q8_cache>(a[0]);
+  ag_q8_cache *to = struct_of<ag_q8_cache>(a[2]);
+  const int32_t *parent = ints_of(a[1], to ? to->B : 0, "parent is not an int32 number for every sequence of dst");
+  int32_t *ref = ref_of(a[3], from);
+  return call([&] { return ag_q8_fork(ctx, s, from, parent, to, ref); });
+}
+
+// cache, ref, which
+AG_BINDING(q8_release, 3) {
+  ag_q8_cache *c = struct_of<ag_q8_cache>(a[0]);
+  int32_t *ref = ref_of(a[1], c);
+  if (THPVariable_Check(a[2]) && (tensor(a[2]).element_size() != 1 || tensor(a[2]).numel() != (c ? c->B : 0)))
+    fail(PyExc_ValueError, "which is not one byte for every sequence");
+  const uint8_t *which = ptr_as<uint8_t>(a[2]);
+  return call([&] { return ag_q8_release(ctx, s, c, ref, which); });
+}
+
+// cache, ref, moved, used
+AG_BINDING(q8_compact_pages, 4) {
+  ag_q8_cache *c = struct_of<ag_q8_cache>(a[0]);
+  int32_t *ref = ref_of(a[1], c), *moved = ref_of(a[2], c), *used = ints_of(a[3], 1, "used is not one int32 number");
+  return call([&] { return ag_q8_compact_pages(ctx, s, c, ref, moved, used); });
+}
+
+// cache, moved
+AG_BINDING(q8_remap, 2) {
+  ag_q8_cache *c = struct_of<ag_q8_cache>(a[0]);
+  const int32_t *moved = ref_of(a[1], c);
+  return call([&] { return ag_q8_remap(ctx, s, c, moved); });
+}
+
 #define AG_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {AG_METHOD(gate), AG_METHOD(rmsnorm_gate), AG_METHOD(compact_kv), AG_METHOD(pack_row_off),
                          AG_METHOD(project_compact_kv), AG_METHOD(prefill_attn), AG_METHOD(compact_prefill_attn),
                          AG_METHOD(decode_attn), AG_METHOD(decode_attn_static), AG_METHOD(recent_fill), AG_METHOD(gate_mha),
                          AG_METHOD(rotate), AG_METHOD(q8_append), AG_METHOD(q8_prefill_attn), AG_METHOD(q8_decode_attn),
+                         AG_METHOD(norm_rotate), AG_METHOD(q8_tree_attn), AG_METHOD(q8_tree_append), AG_METHOD(q8_reserve),
+                         AG_METHOD(q8_fork), AG_METHOD(q8_release), AG_METHOD(q8_compact_pages), AG_METHOD(q8_remap),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "Calls into libag on torch tensors.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};

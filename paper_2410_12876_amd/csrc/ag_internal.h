@@ -11,7 +11,7 @@
 // Kernels that ag_timing_* can time (ids are part of the ABI, see ag_bench.h).
 enum { AG_K_GATE = 0, AG_K_GATE_FINALIZE, AG_K_FLAG_SCAN, AG_K_COMPACT, AG_K_PREFILL, AG_K_DECODE_PARTIAL,
        AG_K_DECODE_MERGE, AG_K_MHA_PROJ, AG_K_MHA_ATTN, AG_K_NORM_GATE, AG_K_ROTATE, AG_K_Q8_FILL, AG_K_Q8_PREFILL,
-       AG_K_Q8_DECODE, AG_K_COUNT };
+       AG_K_Q8_DECODE, AG_K_NORM_ROTATE, AG_K_Q8_TREE, AG_K_Q8_FORK, AG_K_Q8_PAGES, AG_K_COUNT };
 constexpr int kTimerSlots = 1024;  // launches remembered per kernel id
 constexpr int kDecodeMaxUnits = 8192;  // (batch, KV head) units of one decode step
 constexpr int kDecodeArriveGroups = 16, kDecodeArriveStride = 64;  // counters of a step's workgroups, 256 bytes apart
@@ -29,7 +29,7 @@ struct ag_ctx {
   int num_cu;
   char *ws;         // device workspace
   size_t ws_bytes;
-  int32_t *d_err;   // sticky device error word (bit 0: cache capacity overflow, bit 1: position outside a rotation table)
+  int32_t *d_err;   // sticky device error word (bit 0: cache capacity overflow, bit 1: position outside a rotation table, bit 2: node of a tree)
   int32_t *decode_tickets;  // [kDecodeMaxUnits + kDecodeArriveInts] arrival counters of a decode step: zero between launches
   int32_t *prefill_tickets; // [kPrefillTickets] arrival counters of a prefill launch without a flag scan: zero between launches
   char *static_scratch;   // this device's copy of the library's static scratch array (ag_decode_attn_static)

@@ -5,6 +5,7 @@
 #include "ag_internal.h"
 
 constexpr int kQ8Block = AG_Q8_BLOCK;  // rows of a block, and of a page
+constexpr int kQ8TreeMost = AG_Q8_TREE_MOST;  // nodes of a tree
 constexpr int kQ8MinExp = -100;        // least exponent of a block's scale: 2^-e and every value of a page stay normal numbers
 constexpr float kQ8EmptyMax = -3.40282347e+38f;  // reference maximum before any row (no state that holds a row is below it)
 
@@ -50,6 +51,8 @@ struct ag_q8_meta {
 // ---- launchers ----
 hipError_t ag_launch_rotate(ag_ctx *ctx, hipStream_t s, const void *q, const void *k, ag_dtype dt, int B, int Hq, int Hkv, int L,
                             int D, const ag_rope_dev &rope, void *q_out, void *k_out);
+hipError_t ag_launch_norm_rotate(ag_ctx *ctx, hipStream_t s, const void *q, const void *k, ag_dtype dt, int B, int Hq, int Hkv, int L,
+                                 int D, const void *q_weight, const void *k_weight, float eps, const ag_rope_dev &rope, void *q_out, void *k_out);
 
 // Appends the tokens whose flag is set (flags == nullptr: all).  words, blk_off: where the flags' masks and prefix counts go (as from
 // ag_launch_flag_scan; not used without flags).
@@ -58,6 +61,9 @@ hipError_t ag_launch_rotate(ag_ctx *ctx, hipStream_t s, const void *q, const voi
 hipError_t ag_launch_q8_fill(ag_ctx *ctx, hipStream_t s, const void *k, const void *v, const uint8_t *flags, int B, int Hkv, int L, int D,
                              uint64_t *words, int32_t *blk_off, const ag_rope_dev &rope, const ag_q8_dev &cache,
                              uint16_t *tiles, uint32_t *info, ag_q8_meta *meta);
+// Appends, of the at most kQ8TreeMost nodes of every sequence's tree, those above last[b] and itself whose flag is set.
+hipError_t ag_launch_q8_tree_append(ag_ctx *ctx, hipStream_t s, const void *k, const void *v, const uint8_t *flags, const int32_t *parent,
+                                    const int32_t *last, int B, int Hkv, int L, int D, const ag_rope_dev &rope, const ag_q8_dev &cache);
 size_t ag_ws_q8_decode_floats(int num_cu, int G, int D);  // records of a step
 int64_t ag_q8_decode_cost(int64_t units, int max_blocks);  // the largest number that a step's work list can come to; it counts in 32 bits
 hipError_t ag_launch_q8_decode(ag_ctx *ctx, hipStream_t s, const void *q, const void *k_new, const void *v_new, const uint8_t *new_flags,
@@ -76,6 +82,29 @@ int ag_q8_prefill_shorter(int Hq, int Hkv, int L);
 hipError_t ag_launch_q8_prefill(ag_ctx *ctx, hipStream_t s, const void *q, const void *k, const void *v, int B, int Hq, int Hkv, int L,
                                 int D, const uint64_t *words, const int32_t *blk_off, const ag_rope_dev &rope, float scale,
                                 const ag_q8_dev &cache, const ag_q8_prefill_ws &w, void *out);
+
+// ---- trees of drafted tokens (ag_q8_tree.hip) ----
+size_t ag_ws_q8_tree_floats(int num_cu, int rows, int D);                     // records of a call of `rows` query rows a unit
+int64_t ag_q8_tree_cost(int64_t units, int rows, int max_blocks);             // the largest number that its work list can come to; it counts in 32 bits
+hipError_t ag_launch_q8_tree(ag_ctx *ctx, hipStream_t s, const void *q, const void *k, const void *v, const uint8_t *flags, const int32_t *parent,
+                             int B, int Hq, int Hkv, int L, int D, const ag_rope_dev &rope, float scale, const ag_q8_dev &cache, void *out, float *rec);
+
+// ---- pools of pages (ag_q8_pages.hip) ----
+constexpr int kQ8MaxPages = 1 << 25;  // of a pool whose pages are counted
+constexpr int kQ8PageChunk = 4096;    // pages that one workgroup lists
+static inline int ag_q8_page_chunks(int n_pages) { return (n_pages + kQ8PageChunk - 1) / kQ8PageChunk; }
+struct ag_q8_pool_ws {
+  int32_t *list;   // [chunks, kQ8PageChunk] a chunk's pages: those in use in order, then the free ones in order
+  int32_t *count;  // [chunks] free ones
+  int32_t *need;   // [units] pages that a unit is to get
+};
+hipError_t ag_launch_q8_reserve(ag_ctx *ctx, hipStream_t s, int units, const ag_q8_dev &c, int32_t *page, int32_t *ref, int rows, const ag_q8_pool_ws &w);
+hipError_t ag_launch_q8_fork(ag_ctx *ctx, hipStream_t s, const ag_q8_dev &src, int src_B, const int32_t *parent, const ag_q8_dev &dst, int32_t *dst_page,
+                             int B, int Hkv, int D, int32_t *ref);
+hipError_t ag_launch_q8_release(ag_ctx *ctx, hipStream_t s, int B, int Hkv, const ag_q8_dev &c, int32_t *page, int32_t *ref, const uint8_t *which);
+hipError_t ag_launch_q8_compact_pages(ag_ctx *ctx, hipStream_t s, const ag_q8_dev &c, int D, int32_t *ref, int32_t *moved, int32_t *used,
+                                      const ag_q8_pool_ws &w);
+hipError_t ag_launch_q8_remap(ag_ctx *ctx, hipStream_t s, int units, const ag_q8_dev &c, int32_t *page, const int32_t *moved);
 
 // Dynamic LDS above the default limit: raised once per device and kernel, to the most that the kernel can need (a limit that
 // followed each call could be lowered by one thread under another one's launch).
@@ -97,6 +126,7 @@ typedef __attribute__((__vector_size__(2 * sizeof(float)))) float q8_f32x2;
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float q8_f32x4;
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float q8_f32x16;
 typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t q8_u32x4;
+typedef __attribute__((__vector_size__(2 * sizeof(uint32_t)))) uint32_t q8_u32x2;
 typedef __attribute__((__vector_size__(2 * sizeof(int16_t)))) int16_t q8_s16x2;
 typedef __attribute__((__vector_size__(2 * sizeof(uint16_t)))) uint16_t q8_u16x2;
 

@@ -1,4 +1,4 @@
-// C entry points of the rotation and of the paged 8-bit cache: argument validation, workspace carving, kernel sequencing.
+// C entry points of the rotation, of the paged 8-bit cache, of trees over it and of its pool of pages: argument validation, workspace carving, kernel sequencing.
 #include <math.h>
 
 #include <algorithm>
@@ -63,6 +63,24 @@ struct scan_ws {
   uint64_t *words;
   int32_t *blk_off;
 };
+ag_q8_pool_ws take_pool(ws_cursor &ws, int units, int n_pages) {
+  ag_q8_pool_ws w;
+  const size_t chunks = ag_q8_page_chunks(n_pages);
+  w.list = ws.take<int32_t>(chunks * kQ8PageChunk);
+  w.count = ws.take<int32_t>(chunks);
+  w.need = ws.take<int32_t>(units);
+  return w;
+}
+// The checks that the pool's calls share.
+ag_status check_pool(ag_ctx *ctx, const char *who, const ag_q8_cache *c, const int32_t *ref, ag_q8_dev *dev) {
+  const ag_status st = check_q8(ctx, who, c, dev);
+  if (st != AG_OK) return st;
+  AG_REQUIRE(ref, AG_EINVAL, "%s: null pointer", who);
+  AG_REQUIRE(c->n_pages <= kQ8MaxPages, AG_EUNSUPPORTED, "%s: cache: n_pages = %d exceeds %d", who, c->n_pages, kQ8MaxPages);
+  return AG_OK;
+}
+int32_t *table_of(const ag_q8_cache *c) { return const_cast<int32_t *>(c->page); }  // (the pool's calls write it)
+
 scan_ws take_scan(ws_cursor &ws, const uint8_t *flags, int units, int L) {
   scan_ws s{nullptr, nullptr};
   if (!flags) return s;
@@ -186,6 +204,158 @@ ag_status ag_q8_decode_attn(ag_ctx *ctx, void *hip_stream, const void *q, const 
   st = ag_need_device(ctx);
   if (st != AG_OK) return st;
   AG_HIP(ag_launch_q8_decode(ctx, (hipStream_t)hip_stream, q, k_new, v_new, new_flags, cache->B, Hq, cache->Hkv, cache->D, r, scale, c, out, rec));
+  return AG_OK;
+}
+
+ag_status ag_norm_rotate(ag_ctx *ctx, void *hip_stream, const void *q, const void *k, ag_dtype dtype, int B, int Hq, int Hkv, int L,
+                         int D, const void *q_weight, const void *k_weight, float eps, const ag_rope *rope, void *q_out, void *k_out) {
+  if (!ctx) return AG_EINVAL;
+  AG_REQUIRE(q && q_out && q_weight && (k == nullptr) == (k_out == nullptr) && (k == nullptr) == (k_weight == nullptr), AG_EINVAL,
+             "ag_norm_rotate: null pointer");
+  if (!k) Hkv = 0;
+  AG_REQUIRE(B > 0 && Hq > 0 && L > 0 && D > 0 && (!k || Hkv > 0), AG_EINVAL, "ag_norm_rotate: sizes must be positive");
+  AG_REQUIRE(dtype == AG_F32 || dtype == AG_BF16, AG_EINVAL, "ag_norm_rotate: unknown dtype %d", (int)dtype);
+  AG_REQUIRE(eps >= 0x1p-100f && isfinite(eps), AG_EINVAL, "ag_norm_rotate: eps must be finite and at least 2^-100");
+  AG_REQUIRE(D % 16 == 0 && D <= 512, AG_EUNSUPPORTED, "ag_norm_rotate: D = %d (a multiple of 16, at most 512)", D);
+  AG_REQUIRE(L <= kMaxL && (int64_t)B * L < (1ll << 31) && (int64_t)Hq + Hkv <= 65535, AG_EUNSUPPORTED, "ag_norm_rotate: problem too large");
+  AG_REQUIRE(aligned({q, k, q_weight, k_weight, q_out, k_out}), AG_EINVAL, "ag_norm_rotate: tensors must be 16-byte aligned");
+  ag_rope_dev r;
+  ag_status st = check_rope(ctx, "ag_norm_rotate", rope, D, (int64_t)B * L, &r, false);
+  if (st != AG_OK) return st;
+  st = ag_need_device(ctx);
+  if (st != AG_OK) return st;
+  AG_HIP(ag_launch_norm_rotate(ctx, (hipStream_t)hip_stream, q, k, dtype, B, Hq, Hkv, L, D, q_weight, k_weight, eps, r, q_out, k_out));
+  return AG_OK;
+}
+
+size_t ag_q8_tree_workspace_bytes(int B, int L, int Hq, int Hkv, int D, int max_blocks) {
+  if (B <= 0 || L <= 0 || L > kQ8TreeMost || (D != 128 && D != 64) || max_blocks <= 0 || !group_ok(Hq, Hkv) || (int64_t)B * Hkv > kDecodeMaxUnits) return 0;
+  return ag_align256(ag_ws_q8_tree_floats(kMostCu, L * (Hq / Hkv), D) * sizeof(float)) + 4096;
+}
+
+ag_status ag_q8_tree_attn(ag_ctx *ctx, void *hip_stream, const void *q, const void *k, const void *v, const uint8_t *flags,
+                          const int32_t *parent, int L, int Hq, const ag_rope *rope, float scale, const ag_q8_cache *cache, void *out) {
+  if (!ctx) return AG_EINVAL;
+  AG_REQUIRE(q && k && v && parent && out, AG_EINVAL, "ag_q8_tree_attn: null pointer");
+  AG_REQUIRE(L > 0, AG_EINVAL, "ag_q8_tree_attn: L must be positive");
+  AG_REQUIRE(L <= kQ8TreeMost, AG_EUNSUPPORTED, "ag_q8_tree_attn: L = %d exceeds %d", L, kQ8TreeMost);
+  AG_REQUIRE(scale > 0.f && isfinite(scale), AG_EINVAL, "ag_q8_tree_attn: scale must be positive and finite");
+  ag_q8_dev c;
+  ag_status st = check_q8(ctx, "ag_q8_tree_attn", cache, &c);
+  if (st != AG_OK) return st;
+  AG_REQUIRE(Hq > 0 && Hq % cache->Hkv == 0, AG_EINVAL, "ag_q8_tree_attn: Hq must be a positive multiple of Hkv");
+  AG_REQUIRE(group_ok(Hq, cache->Hkv), AG_EUNSUPPORTED, "ag_q8_tree_attn: %d query heads per KV head", Hq / cache->Hkv);
+  AG_REQUIRE(aligned({q, k, v, out}), AG_EINVAL, "ag_q8_tree_attn: tensors must be 16-byte aligned");
+  const int units = cache->B * cache->Hkv, rows = L * (Hq / cache->Hkv);
+  AG_REQUIRE(ag_q8_tree_cost(units, rows, cache->max_blocks) < (1ll << 31), AG_EUNSUPPORTED,
+             "ag_q8_tree_attn: cache: %d units of max_blocks = %d are too many", units, cache->max_blocks);
+  ag_rope_dev r;
+  st = check_rope(ctx, "ag_q8_tree_attn", rope, cache->D, (int64_t)cache->B * L, &r);
+  if (st != AG_OK) return st;
+  ws_cursor ws{ctx->ws, ctx->ws_bytes, 0, true};
+  float *rec = ws.take<float>(ag_ws_q8_tree_floats(ctx->num_cu, rows, cache->D));
+  AG_REQUIRE(ws.ok, AG_EWORKSPACE, "ag_q8_tree_attn: workspace of %zu bytes is too small (need %zu)", ctx->ws_bytes, ws.off);
+  st = ag_need_device(ctx);
+  if (st != AG_OK) return st;
+  AG_HIP(ag_launch_q8_tree(ctx, (hipStream_t)hip_stream, q, k, v, flags, parent, cache->B, Hq, cache->Hkv, L, cache->D, r, scale, c, out, rec));
+  return AG_OK;
+}
+
+ag_status ag_q8_tree_append(ag_ctx *ctx, void *hip_stream, const void *k, const void *v, const uint8_t *flags, const int32_t *parent,
+                            const int32_t *last, int L, const ag_rope *rope, ag_q8_cache *cache) {
+  if (!ctx) return AG_EINVAL;
+  AG_REQUIRE(k && v && parent && last, AG_EINVAL, "ag_q8_tree_append: null pointer");
+  AG_REQUIRE(L > 0, AG_EINVAL, "ag_q8_tree_append: L must be positive");
+  AG_REQUIRE(L <= kQ8TreeMost, AG_EUNSUPPORTED, "ag_q8_tree_append: L = %d exceeds %d", L, kQ8TreeMost);
+  ag_q8_dev c;
+  ag_status st = check_q8(ctx, "ag_q8_tree_append", cache, &c);
+  if (st != AG_OK) return st;
+  AG_REQUIRE(aligned({k, v}), AG_EINVAL, "ag_q8_tree_append: k and v must be 16-byte aligned");
+  ag_rope_dev r;
+  st = check_rope(ctx, "ag_q8_tree_append", rope, cache->D, (int64_t)cache->B * L, &r);
+  if (st != AG_OK) return st;
+  st = ag_need_device(ctx);
+  if (st != AG_OK) return st;
+  AG_HIP(ag_launch_q8_tree_append(ctx, (hipStream_t)hip_stream, k, v, flags, parent, last, cache->B, cache->Hkv, L, cache->D, r, c));
+  return AG_OK;
+}
+
+size_t ag_q8_pool_workspace_bytes(int B, int Hkv, int n_pages) {
+  if (B <= 0 || Hkv <= 0 || (int64_t)B * Hkv > kDecodeMaxUnits || n_pages <= 0 || n_pages > kQ8MaxPages) return 0;
+  ws_cursor ws{nullptr, ~size_t(0) >> 1, 0, true};
+  take_pool(ws, B * Hkv, n_pages);
+  return ws.off + 4096;
+}
+
+ag_status ag_q8_reserve(ag_ctx *ctx, void *hip_stream, ag_q8_cache *cache, int32_t *ref, int rows) {
+  if (!ctx) return AG_EINVAL;
+  ag_q8_dev c;
+  ag_status st = check_pool(ctx, "ag_q8_reserve", cache, ref, &c);
+  if (st != AG_OK) return st;
+  AG_REQUIRE(rows >= 0, AG_EINVAL, "ag_q8_reserve: rows is negative");
+  const int units = cache->B * cache->Hkv;
+  ws_cursor ws{ctx->ws, ctx->ws_bytes, 0, true};
+  const ag_q8_pool_ws w = take_pool(ws, units, cache->n_pages);
+  AG_REQUIRE(ws.ok, AG_EWORKSPACE, "ag_q8_reserve: workspace of %zu bytes is too small (need %zu)", ctx->ws_bytes, ws.off);
+  st = ag_need_device(ctx);
+  if (st != AG_OK) return st;
+  AG_HIP(ag_launch_q8_reserve(ctx, (hipStream_t)hip_stream, units, c, table_of(cache), ref, rows, w));
+  return AG_OK;
+}
+
+ag_status ag_q8_fork(ag_ctx *ctx, void *hip_stream, const ag_q8_cache *src, const int32_t *parent, ag_q8_cache *dst, int32_t *ref) {
+  if (!ctx) return AG_EINVAL;
+  ag_q8_dev from, to;
+  ag_status st = check_pool(ctx, "ag_q8_fork", src, ref, &from);
+  if (st == AG_OK) st = check_pool(ctx, "ag_q8_fork", dst, ref, &to);
+  if (st != AG_OK) return st;
+  AG_REQUIRE(parent, AG_EINVAL, "ag_q8_fork: null pointer");
+  AG_REQUIRE(src->k == dst->k && src->v == dst->v && src->k_scale == dst->k_scale && src->v_scale == dst->v_scale && src->n_pages == dst->n_pages,
+             AG_EINVAL, "ag_q8_fork: src and dst are not caches over one pool");
+  AG_REQUIRE(src->Hkv == dst->Hkv && src->D == dst->D, AG_EINVAL, "ag_q8_fork: src and dst differ in their heads");
+  AG_REQUIRE(dst->max_blocks >= src->max_blocks, AG_EINVAL, "ag_q8_fork: dst's table is shorter than src's");
+  AG_REQUIRE(src->page != dst->page && src->len != dst->len && src->k_tail != dst->k_tail && src->v_tail != dst->v_tail, AG_EINVAL,
+             "ag_q8_fork: src and dst share a table, lengths or tails");
+  st = ag_need_device(ctx);
+  if (st != AG_OK) return st;
+  AG_HIP(ag_launch_q8_fork(ctx, (hipStream_t)hip_stream, from, src->B, parent, to, table_of(dst), dst->B, dst->Hkv, dst->D, ref));
+  return AG_OK;
+}
+
+ag_status ag_q8_release(ag_ctx *ctx, void *hip_stream, ag_q8_cache *cache, int32_t *ref, const uint8_t *which) {
+  if (!ctx) return AG_EINVAL;
+  ag_q8_dev c;
+  ag_status st = check_pool(ctx, "ag_q8_release", cache, ref, &c);
+  if (st != AG_OK) return st;
+  st = ag_need_device(ctx);
+  if (st != AG_OK) return st;
+  AG_HIP(ag_launch_q8_release(ctx, (hipStream_t)hip_stream, cache->B, cache->Hkv, c, table_of(cache), ref, which));
+  return AG_OK;
+}
+
+ag_status ag_q8_compact_pages(ag_ctx *ctx, void *hip_stream, ag_q8_cache *cache, int32_t *ref, int32_t *moved, int32_t *used) {
+  if (!ctx) return AG_EINVAL;
+  ag_q8_dev c;
+  ag_status st = check_pool(ctx, "ag_q8_compact_pages", cache, ref, &c);
+  if (st != AG_OK) return st;
+  AG_REQUIRE(moved && used, AG_EINVAL, "ag_q8_compact_pages: null pointer");
+  ws_cursor ws{ctx->ws, ctx->ws_bytes, 0, true};
+  const ag_q8_pool_ws w = take_pool(ws, 1, cache->n_pages);
+  AG_REQUIRE(ws.ok, AG_EWORKSPACE, "ag_q8_compact_pages: workspace of %zu bytes is too small (need %zu)", ctx->ws_bytes, ws.off);
+  st = ag_need_device(ctx);
+  if (st != AG_OK) return st;
+  AG_HIP(ag_launch_q8_compact_pages(ctx, (hipStream_t)hip_stream, c, cache->D, ref, moved, used, w));
+  return AG_OK;
+}
+
+ag_status ag_q8_remap(ag_ctx *ctx, void *hip_stream, ag_q8_cache *cache, const int32_t *moved) {
+  if (!ctx) return AG_EINVAL;
+  ag_q8_dev c;
+  ag_status st = check_pool(ctx, "ag_q8_remap", cache, moved, &c);
+  if (st != AG_OK) return st;
+  st = ag_need_device(ctx);
+  if (st != AG_OK) return st;
+  AG_HIP(ag_launch_q8_remap(ctx, (hipStream_t)hip_stream, cache->B * cache->Hkv, c, table_of(cache), moved));
   return AG_OK;
 }
 

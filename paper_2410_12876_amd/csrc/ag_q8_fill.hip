@@ -38,6 +38,7 @@ struct fill_args {
   ag_q8_meta *meta;
   int32_t *arrived;  // [units] zero between launches
   int32_t *err;
+  const int32_t *parent, *last;  // PATH: [B, L], [B]
   int Hkv, L, nw, n_blk;
 };
 
@@ -58,8 +59,44 @@ __device__ __forceinline__ uint32_t flag_bits(const uint8_t *f, int t, int L) {
   return bits;
 }
 
+// The nodes above node `last` of a tree of L <= kQ8TreeMost nodes, and itself, as bits: word i has nodes 64 i ...  Every lane holds the parents
+// of nodes lane, 64 + lane, ...; the walk is the wave's.  (A parent is before its node, so the walk ends.)
+struct path_bits {
+  uint64_t w[kQ8TreeMost / 64];
+};
+__device__ __forceinline__ path_bits path_of(const int32_t *parent, int last, int L, int lane, int32_t *err) {
+  constexpr int N = kQ8TreeMost / 64;
+  path_bits b;
+  int up[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    b.w[i] = 0;
+    up[i] = 64 * i + lane < L ? parent[64 * i + lane] : -1;
+  }
+  int at = __builtin_amdgcn_readfirstlane(last);
+  bool bad = at >= L;
+  if (bad) at = -1;
+  while (at >= 0) {
+    int next = -1;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (at >> 6 == i) {
+        b.w[i] |= 1ull << (at & 63);
+        next = __builtin_amdgcn_readlane(up[i], at & 63);
+      }
+    if (next >= at) {
+      bad = true;
+      next = -1;
+    }
+    at = next;
+  }
+  if (bad && lane == 0) atomicOr(err, 4);
+  return b;
+}
+
 // CHUNKS: pieces of 16 flags that a thread reads (the workgroup: all of the unit's); 0: they are taken from words and blk_off.
-template <int D, bool TILES, int CHUNKS>
+// PATH: only tokens on the accepted path of a tree are kept (L <= kQ8TreeMost, CHUNKS = 1).
+template <int D, bool TILES, int CHUNKS, bool PATH>
 __global__ __launch_bounds__(4 * D, 4) void ag_q8_fill_kernel(fill_args a) {
   constexpr int T = 4 * D, WAVES = T / 64;  // threads: 16 values of a row each
   constexpr int RS = D + 8;                 // values per row of V in LDS (rows 4 apart start 16 banks apart)
@@ -83,6 +120,15 @@ __global__ __launch_bounds__(4 * D, 4) void ag_q8_fill_kernel(fill_args a) {
       bits[i] = a.flags ? (left > 0 ? flag_bits(a.flags + (size_t)u * a.L, t + 16 * i, a.L) : 0u) : (left >= 16 ? 0xffffu : (1u << max(left, 0)) - 1u);
       mine += __popc(bits[i]);
     }
+  }
+  if constexpr (PATH) {
+    const int b = u / a.Hkv;
+    const path_bits path = path_of(a.parent + (size_t)b * a.L, a.last[b], a.L, lane, a.err);
+    uint64_t word = 0;
+#pragma unroll
+    for (int i = 0; i < kQ8TreeMost / 64; ++i) word = tid / 4 == i ? path.w[i] : word;
+    bits[0] &= (uint32_t)(word >> (tid % 4 * 16)) & 0xffffu;
+    mine = __popc(bits[0]);
   }
   if (tid == 0) s_stop = 0x7fffffff;
   if (tid < 3) {
@@ -399,7 +445,7 @@ hipError_t ag_launch_q8_fill(ag_ctx *ctx, hipStream_t s, const void *k, const vo
                              uint64_t *words, int32_t *blk_off, const ag_rope_dev &rope, const ag_q8_dev &cache,
                              uint16_t *tiles, uint32_t *info, ag_q8_meta *meta) {
   fill_args a;
-  a.k = (const uint16_t *)k; a.v = (const uint16_t *)v; a.flags = flags;
+  a.k = (const uint16_t *)k; a.v = (const uint16_t *)v; a.flags = flags; a.parent = a.last = nullptr;
   a.words = words; a.blk_off = blk_off; a.c = cache; a.rope = rope;
   a.tiles = tiles; a.info = info; a.meta = meta;
   a.arrived = ctx->decode_tickets; a.err = ctx->d_err;
@@ -409,7 +455,7 @@ hipError_t ag_launch_q8_fill(ag_ctx *ctx, hipStream_t s, const void *k, const vo
     const hipError_t e = ag_launch_flag_scan(ctx, s, flags, B * Hkv, L, words, blk_off, nullptr);
     if (e != hipSuccess) return e;
   }
-#define AG_FILL(DD, TT, CC) AG_LAUNCH(ag_time_kernel(ctx, AG_K_Q8_FILL), (ag_q8_fill_kernel<DD, TT, CC>), grid, block, 0, s, a)
+#define AG_FILL(DD, TT, CC) AG_LAUNCH(ag_time_kernel(ctx, AG_K_Q8_FILL), (ag_q8_fill_kernel<DD, TT, CC, false>), grid, block, 0, s, a)
 #define AG_FILL_C(DD, TT)                                                          \
   do {                                                                             \
     if (L <= 16 * 4 * DD) AG_FILL(DD, TT, 1);                                      \
@@ -422,5 +468,19 @@ hipError_t ag_launch_q8_fill(ag_ctx *ctx, hipStream_t s, const void *k, const vo
   else AG_FILL_C(64, false);
 #undef AG_FILL_C
 #undef AG_FILL
+  return hipGetLastError();
+}
+
+hipError_t ag_launch_q8_tree_append(ag_ctx *ctx, hipStream_t s, const void *k, const void *v, const uint8_t *flags, const int32_t *parent,
+                                    const int32_t *last, int B, int Hkv, int L, int D, const ag_rope_dev &rope, const ag_q8_dev &cache) {
+  fill_args a;
+  a.k = (const uint16_t *)k; a.v = (const uint16_t *)v; a.flags = flags; a.parent = parent; a.last = last;
+  a.words = nullptr; a.blk_off = nullptr; a.c = cache; a.rope = rope;
+  a.tiles = nullptr; a.info = nullptr; a.meta = nullptr;
+  a.arrived = ctx->decode_tickets; a.err = ctx->d_err;
+  a.Hkv = Hkv; a.L = L; a.nw = ag_nwords(L); a.n_blk = ag_q8_fill_blocks(L);
+  const dim3 grid(std::min(a.n_blk, std::max(1, kFillWg * ctx->num_cu / (B * Hkv))), B * Hkv), block(4 * D);
+  if (D == 128) AG_LAUNCH(ag_time_kernel(ctx, AG_K_Q8_FILL), (ag_q8_fill_kernel<128, false, 1, true>), grid, block, 0, s, a);
+  else AG_LAUNCH(ag_time_kernel(ctx, AG_K_Q8_FILL), (ag_q8_fill_kernel<64, false, 1, true>), grid, block, 0, s, a);
   return hipGetLastError();
 }

@@ -1,0 +1,311 @@
+// A pool of pages that several caches share: pages counted by the table entries that name them, handed out, shared, given back, moved together.
+//
+// Everything is decided by the counts and the tables as they stand before a launch, in the order of page, unit and block numbers, so the
+// result does not depend on timing; counts change by integer atomics, whose order does not matter.
+//   * ag_q8_fork_kernel, one launch: a workgroup per unit copies the tails (2 x 128 D bytes in and out; what bounds a large fork is that
+//     copy, a small one the chain parent -> length -> table -> count) and counts the entries.
+//   * Who gets which page needs the free pages' ranks.  ag_q8_list_kernel lists, for every 4096 pages, those in use and then the free ones, and counts; the
+//     second launch finds the chunk of a rank by a search over the counts' prefix sums.  (Taking both from the counts themselves would make
+//     one launch read what another one of its workgroups changes.)
+//   * ag_q8_move_kernel: source i is the i-th page in use behind N, destination i the i-th free page before it, so no page is both.
+#include <algorithm>
+
+#include "ag_q8.h"
+
+namespace {
+
+constexpr int kListThreads = 1024;
+constexpr int kThreads = 256;
+constexpr int kUnitsAWg = kThreads / 64;  // a wave per unit
+
+// Over a workgroup of N waves: exclusive prefix sum and total.  Two barriers.
+template <int N> __device__ __forceinline__ int wg_prefix(int x, int &total, int32_t *sums) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int sum, at = ag_wave_prefix(x, sum);
+  __syncthreads();
+  if (lane == 0) sums[wave] = sum;
+  __syncthreads();
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < N; ++w) {
+    if (w < wave) at += sums[w];
+    total += sums[w];
+  }
+  return at;
+}
+
+struct blocks {
+  int first, end, table;  // blocks that are to have pages; the table's
+};
+__device__ __forceinline__ blocks wanted(const ag_q8_dev &c, int u, int rows) {
+  const int most = c.max_blocks * kQ8Block + kQ8Block - 1, n = max(0, min(c.len[u], most));
+  const int end = (int)(((int64_t)n + rows) / kQ8Block);
+  return blocks{n / kQ8Block, min(end, c.max_blocks), end};
+}
+
+// Workgroups [0, chunks): the chunk's pages listed, those in use first; the others (rows >= 0): the pages that their units want.
+__global__ __launch_bounds__(kListThreads) void ag_q8_list_kernel(ag_q8_dev c, const int32_t *page, const int32_t *ref, int chunks, int U, int rows,
+                                                                   ag_q8_pool_ws w, int32_t *err) {
+  __shared__ int32_t sums[kListThreads / 64];
+  const int tid = threadIdx.x, lane = tid & 63;
+  if ((int)blockIdx.x >= chunks) {
+    const int u = ((int)blockIdx.x - chunks) * (kListThreads / 64) + (tid >> 6);
+    if (u >= U) return;
+    const blocks b = wanted(c, u, rows);
+    int n = 0;
+    for (int j = b.first + lane; j < b.end; j += 64) n += (uint32_t)page[(size_t)u * c.max_blocks + j] >= (uint32_t)c.n_pages;
+    int total;
+    ag_wave_prefix(n, total);
+    if (lane == 0) {
+      w.need[u] = total;
+      if (b.table > c.max_blocks) atomicOr(err, 1);
+    }
+    return;
+  }
+  const int chunk = blockIdx.x, first = chunk * kQ8PageChunk, p = first + 4 * tid, here = min(kQ8PageChunk, c.n_pages - first);
+  int r[4];
+  int n_used = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    r[i] = p + i < c.n_pages ? ref[p + i] : 0;
+    n_used += r[i] != 0;
+  }
+  int total, at = wg_prefix<kListThreads / 64>(n_used, total, sums);
+  int32_t *list = w.list + (size_t)first;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (p + i < c.n_pages) {
+      if (r[i] != 0) list[at++] = p + i;
+      else list[total + (4 * tid + i - at)] = p + i;
+    }
+  if (tid == 0) w.count[chunk] = here - total;
+}
+
+// s_pre[i] = free pages before chunk i, i <= chunks.
+template <int N> __device__ __forceinline__ void free_before(const int32_t *count, int chunks, int32_t *s_pre, int32_t *sums) {
+  int before = 0;
+  for (int i0 = 0; i0 < chunks; i0 += 64 * N) {
+    const int i = i0 + (int)threadIdx.x;
+    int total;
+    const int at = wg_prefix<N>(i < chunks ? count[i] : 0, total, sums);
+    if (i < chunks) s_pre[i] = before + at;
+    before += total;
+  }
+  if (threadIdx.x == 0) s_pre[chunks] = before;
+  __syncthreads();
+}
+// The chunk that holds element k, of those of which before(i) are ahead of chunk i: the last one with before(i) <= k.
+template <typename F> __device__ __forceinline__ int chunk_of(F &&before, int chunks, int k) {
+  int lo = 0, hi = chunks - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (before(mid) <= k) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
+}
+__device__ __forceinline__ int free_page(const ag_q8_pool_ws &w, const int32_t *s_pre, int chunks, int n_pages, int k) {
+  const int i = chunk_of([&](int x) { return s_pre[x]; }, chunks, k), here = min(kQ8PageChunk, n_pages - i * kQ8PageChunk);
+  return w.list[(size_t)i * kQ8PageChunk + here - (s_pre[i + 1] - s_pre[i]) + k - s_pre[i]];
+}
+__device__ __forceinline__ int used_page(const ag_q8_pool_ws &w, const int32_t *s_pre, int chunks, int k) {
+  auto before = [&](int x) { return x * kQ8PageChunk - s_pre[x]; };
+  const int i = chunk_of(before, chunks, k);
+  return w.list[(size_t)i * kQ8PageChunk + k - before(i)];
+}
+
+// A wave per unit: the blocks without a page take the free pages from the unit's rank on.
+__global__ __launch_bounds__(kThreads) void ag_q8_reserve_kernel(ag_q8_dev c, int32_t *page, int32_t *ref, int chunks, int U, int rows,
+                                                                  ag_q8_pool_ws w, int32_t *err) {
+  extern __shared__ int32_t s_pre[];  // [chunks + 1]
+  __shared__ int32_t sums[kUnitsAWg];
+  const int tid = threadIdx.x, lane = tid & 63, u0 = blockIdx.x * kUnitsAWg, u = u0 + (tid >> 6);
+  int before = 0, total;
+  for (int i = tid; i < u0; i += kThreads) before += w.need[i];
+  wg_prefix<kUnitsAWg>(before, total, sums);
+  free_before<kUnitsAWg>(w.count, chunks, s_pre, sums);
+  if (u >= U) return;
+  int rank = total;
+  for (int i = u0; i < u; ++i) rank += w.need[i];
+  if (w.need[u] == 0) return;
+  const int there = s_pre[chunks];
+  const blocks b = wanted(c, u, rows);
+  bool out = false;
+  for (int j0 = b.first; j0 < b.end; j0 += 64) {
+    const int j = j0 + lane;
+    int32_t *entry = page + (size_t)u * c.max_blocks + j;
+    const bool mine = j < b.end && (uint32_t)*entry >= (uint32_t)c.n_pages;
+    int n, k = rank + ag_wave_prefix(mine, n);
+    if (mine && k < there) {
+      const int p = free_page(w, s_pre, chunks, c.n_pages, k);
+      *entry = p;
+      ref[p] = 1;
+    }
+    out |= mine && k >= there;
+    rank += n;
+  }
+  if (out) atomicOr(err, 1);
+}
+
+template <int D>
+__global__ __launch_bounds__(kThreads) void ag_q8_fork_kernel(ag_q8_dev src, int src_B, const int32_t *parent, ag_q8_dev dst, int32_t *page, int Hkv, int32_t *ref) {
+  constexpr int N = kQ8Block * D * 2 / 16 / kThreads;  // 16-byte pieces of a tail per thread
+  const int u = blockIdx.x, tid = threadIdx.x, b = u / Hkv, from = parent[b];
+  const bool some = (uint32_t)from < (uint32_t)src_B;
+  const int v = some ? from * Hkv + u % Hkv : 0;
+  q8_u32x4 k[N], x[N];
+  if (some) {
+    const q8_u32x4 *sk = reinterpret_cast<const q8_u32x4 *>(src.k_tail + (size_t)v * kQ8Block * D) + tid;
+    const q8_u32x4 *sv = reinterpret_cast<const q8_u32x4 *>(src.v_tail + (size_t)v * kQ8Block * D) + tid;
+#pragma unroll
+    for (int i = 0; i < N; ++i) k[i] = sk[i * kThreads];
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = sv[i * kThreads];
+  }
+  const int most = src.max_blocks * kQ8Block + kQ8Block - 1, n = some ? max(0, min(src.len[v], most)) : 0, full = n / kQ8Block;
+  for (int j = tid; j < dst.max_blocks; j += kThreads) {
+    int32_t *entry = page + (size_t)u * dst.max_blocks + j;
+    const int old = *entry;
+    int now = -1;
+    if (j < full) {
+      now = src.page[(size_t)v * src.max_blocks + j];
+      if ((uint32_t)now >= (uint32_t)dst.n_pages) now = -1;
+    }
+    if (now != old) {
+      if ((uint32_t)old < (uint32_t)dst.n_pages) atomicSub(ref + old, 1);
+      if (now >= 0) atomicAdd(ref + now, 1);
+      *entry = now;
+    }
+  }
+  if (tid == 0) dst.len[u] = n;
+  if (!some) return;
+  q8_u32x4 *dk = reinterpret_cast<q8_u32x4 *>(dst.k_tail + (size_t)u * kQ8Block * D) + tid;
+  q8_u32x4 *dv = reinterpret_cast<q8_u32x4 *>(dst.v_tail + (size_t)u * kQ8Block * D) + tid;
+#pragma unroll
+  for (int i = 0; i < N; ++i) dk[i * kThreads] = k[i];
+#pragma unroll
+  for (int i = 0; i < N; ++i) dv[i * kThreads] = x[i];
+}
+
+__global__ __launch_bounds__(kThreads) void ag_q8_release_kernel(ag_q8_dev c, int32_t *page, int Hkv, int32_t *ref, const uint8_t *which) {
+  const int u = blockIdx.x;
+  if (which && which[u / Hkv] == 0) return;
+  for (int j = threadIdx.x; j < c.max_blocks; j += kThreads) {
+    int32_t *entry = page + (size_t)u * c.max_blocks + j;
+    const int p = *entry;
+    if ((uint32_t)p < (uint32_t)c.n_pages) atomicSub(ref + p, 1);
+    *entry = -1;
+  }
+  if (threadIdx.x == 0) c.len[u] = 0;
+}
+
+// Every workgroup takes every n-th of the pages that move, and of the pages whose new number is to be written down.
+template <int D>
+__global__ __launch_bounds__(kThreads) void ag_q8_move_kernel(ag_q8_dev c, int32_t *ref, int32_t *moved, int32_t *used, int chunks, ag_q8_pool_ws w) {
+  extern __shared__ int32_t s_pre[];
+  __shared__ int32_t sums[kThreads / 64];
+  const int tid = threadIdx.x;
+  free_before<kThreads / 64>(w.count, chunks, s_pre, sums);
+  const int N = c.n_pages - s_pre[chunks];  // pages in use
+  // free pages before N: those of the chunks ahead of N's, and of its own list those below N
+  int holes = 0;
+  if (N < c.n_pages) {
+    const int i = N / kQ8PageChunk, here = min(kQ8PageChunk, c.n_pages - i * kQ8PageChunk), n = s_pre[i + 1] - s_pre[i];
+    const int32_t *list = w.list + (size_t)i * kQ8PageChunk + here - n;
+    int lo = 0, hi = n;  // the first one that is not below N
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (list[mid] < N) lo = mid + 1;
+      else hi = mid;
+    }
+    holes = s_pre[i] + lo;
+  }
+  if (blockIdx.x == 0 && tid == 0) used[0] = N;
+  for (int64_t x = (int64_t)blockIdx.x * kThreads + tid; x < c.n_pages; x += (int64_t)gridDim.x * kThreads) {
+    const int i = (int)x / kQ8PageChunk, at = (int)x % kQ8PageChunk, here = min(kQ8PageChunk, c.n_pages - i * kQ8PageChunk);
+    const int p = w.list[x], n_used = here - (s_pre[i + 1] - s_pre[i]);
+    if (at >= n_used) {
+      moved[p] = -1;
+    } else if (p < N) {
+      moved[p] = p;
+    } else {
+      const int k = i * kQ8PageChunk - s_pre[i] + at - (N - holes), to = free_page(w, s_pre, chunks, c.n_pages, k);
+      moved[p] = to;
+      ref[to] = ref[p];
+      ref[p] = 0;
+      c.k_scale[to] = c.k_scale[p];
+      c.v_scale[to] = c.v_scale[p];
+    }
+  }
+  constexpr int P = kQ8Block * D / 16 / kThreads;  // 16-byte pieces of a page per thread
+  for (int k = blockIdx.x; k < holes; k += gridDim.x) {
+    const size_t p = used_page(w, s_pre, chunks, N - holes + k), to = free_page(w, s_pre, chunks, c.n_pages, k);
+    q8_u32x4 a[P], b[P];
+    const q8_u32x4 *pk = reinterpret_cast<const q8_u32x4 *>(c.k + p * kQ8Block * D) + tid, *pv = reinterpret_cast<const q8_u32x4 *>(c.v + p * kQ8Block * D) + tid;
+#pragma unroll
+    for (int i = 0; i < P; ++i) a[i] = pk[i * kThreads];
+#pragma unroll
+    for (int i = 0; i < P; ++i) b[i] = pv[i * kThreads];
+    q8_u32x4 *tk = reinterpret_cast<q8_u32x4 *>(c.k + to * kQ8Block * D) + tid, *tv = reinterpret_cast<q8_u32x4 *>(c.v + to * kQ8Block * D) + tid;
+#pragma unroll
+    for (int i = 0; i < P; ++i) tk[i * kThreads] = a[i];
+#pragma unroll
+    for (int i = 0; i < P; ++i) tv[i * kThreads] = b[i];
+  }
+}
+
+__global__ __launch_bounds__(kThreads) void ag_q8_remap_kernel(int32_t *page, int64_t n, int n_pages, const int32_t *moved) {
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kThreads) {
+    const int p = page[i];
+    if ((uint32_t)p < (uint32_t)n_pages) page[i] = moved[p];
+  }
+}
+
+hipError_t launch_list(ag_ctx *ctx, hipStream_t s, const ag_q8_dev &c, const int32_t *page, const int32_t *ref, int U, int rows, const ag_q8_pool_ws &w) {
+  const int chunks = ag_q8_page_chunks(c.n_pages), per = kListThreads / 64;
+  AG_LAUNCH(ag_time_kernel(ctx, AG_K_Q8_PAGES), ag_q8_list_kernel, dim3(chunks + (U + per - 1) / per), dim3(kListThreads), 0, s, c, page, ref, chunks, U,
+            rows, w, ctx->d_err);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t ag_launch_q8_reserve(ag_ctx *ctx, hipStream_t s, int units, const ag_q8_dev &c, int32_t *page, int32_t *ref, int rows, const ag_q8_pool_ws &w) {
+  const hipError_t e = launch_list(ctx, s, c, page, ref, units, rows, w);
+  if (e != hipSuccess) return e;
+  const int chunks = ag_q8_page_chunks(c.n_pages);
+  AG_LAUNCH(ag_time_kernel(ctx, AG_K_Q8_PAGES), ag_q8_reserve_kernel, dim3((units + kUnitsAWg - 1) / kUnitsAWg), dim3(kThreads), (size_t)(chunks + 1) * 4, s,
+            c, page, ref, chunks, units, rows, w, ctx->d_err);
+  return hipGetLastError();
+}
+
+hipError_t ag_launch_q8_fork(ag_ctx *ctx, hipStream_t s, const ag_q8_dev &src, int src_B, const int32_t *parent, const ag_q8_dev &dst, int32_t *dst_page,
+                             int B, int Hkv, int D, int32_t *ref) {
+  const dim3 grid(B * Hkv);
+  if (D == 128) AG_LAUNCH(ag_time_kernel(ctx, AG_K_Q8_FORK), ag_q8_fork_kernel<128>, grid, dim3(kThreads), 0, s, src, src_B, parent, dst, dst_page, Hkv, ref);
+  else AG_LAUNCH(ag_time_kernel(ctx, AG_K_Q8_FORK), ag_q8_fork_kernel<64>, grid, dim3(kThreads), 0, s, src, src_B, parent, dst, dst_page, Hkv, ref);
+  return hipGetLastError();
+}
+
+hipError_t ag_launch_q8_release(ag_ctx *ctx, hipStream_t s, int B, int Hkv, const ag_q8_dev &c, int32_t *page, int32_t *ref, const uint8_t *which) {
+  AG_LAUNCH(ag_time_kernel(ctx, AG_K_Q8_PAGES), ag_q8_release_kernel, dim3(B * Hkv), dim3(kThreads), 0, s, c, page, Hkv, ref, which);
+  return hipGetLastError();
+}
+
+hipError_t ag_launch_q8_compact_pages(ag_ctx *ctx, hipStream_t s, const ag_q8_dev &c, int D, int32_t *ref, int32_t *moved, int32_t *used,
+                                      const ag_q8_pool_ws &w) {
+  const hipError_t e = launch_list(ctx, s, c, nullptr, ref, 0, 0, w);
+  if (e != hipSuccess) return e;
+  const int chunks = ag_q8_page_chunks(c.n_pages), grid = std::min(c.n_pages, 8 * ctx->num_cu);
+  const size_t lds = (size_t)(chunks + 1) * 4;
+  if (D == 128) AG_LAUNCH(ag_time_kernel(ctx, AG_K_Q8_PAGES), ag_q8_move_kernel<128>, dim3(grid), dim3(kThreads), lds, s, c, ref, moved, used, chunks, w);
+  else AG_LAUNCH(ag_time_kernel(ctx, AG_K_Q8_PAGES), ag_q8_move_kernel<64>, dim3(grid), dim3(kThreads), lds, s, c, ref, moved, used, chunks, w);
+  return hipGetLastError();
+}
+
+hipError_t ag_launch_q8_remap(ag_ctx *ctx, hipStream_t s, int units, const ag_q8_dev &c, int32_t *page, const int32_t *moved) {
+  const int64_t n = (int64_t)units * c.max_blocks;
+  const int grid = (int)std::min<int64_t>((n + kThreads - 1) / kThreads, 8 * ctx->num_cu);
+  AG_LAUNCH(ag_time_kernel(ctx, AG_K_Q8_PAGES), ag_q8_remap_kernel, dim3(grid), dim3(kThreads), 0, s, page, n, c.n_pages, moved);
+  return hipGetLastError();
+}

@@ -84,6 +84,94 @@ __global__ __launch_bounds__(256) void ag_rotate_kernel(const T *q, const T *k, 
   }
 }
 
+// Every head's vector normalised by its root mean square and turned, y = turn(x r w), in one pass.  Bound by memory as the rotation is.
+// A vector's pieces are `lanes` (a power of two) neighbouring lanes': the squares of a piece and of its partner are added up in a lane, then
+// over the group.  Sums are in 32 bits; where one passes their range (values from 2^60 on) the vector is taken 2^-70 as large.
+template <typename T>
+__global__ __launch_bounds__(256) void ag_norm_rotate_kernel(const T *q, const T *k, T *q_out, T *k_out, const T *q_weight, const T *k_weight,
+                                                             float eps, int tokens, int Hq, int Hkv, int L, int D, int lanes_log, int heads,
+                                                             ag_rope_dev rope, int32_t *err) {
+  constexpr int E = 16 / sizeof(T);  // values of a piece
+  constexpr float kSmall = 8.470329473e-22f;  // 2^-70
+  const int lanes = 1 << lanes_log;
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t token = id >> lanes_log;
+  const int piece = (int)id & (lanes - 1), i = piece * E;
+  const bool there = token < tokens && i < D / 2;  // (the other lanes take part in the sums)
+  const int n = there ? (int)token : 0, at_i = there ? i : 0;
+  const int b = n / L, t = n - b * L;
+  float c[E], s[E];
+  if (rope.table) {
+    const q8_rows at = q8_rope_rows(rope, n, err);
+#pragma unroll
+    for (int j = 0; j < E; j += 4) {
+      if (rope.quads) {
+        const q8_angles e = q8_angles4(rope, at, at_i + j, D);
+        c[j] = e.c.x; c[j + 1] = e.c.y; c[j + 2] = e.c.z; c[j + 3] = e.c.w;
+        s[j] = e.s.x; s[j + 1] = e.s.y; s[j + 2] = e.s.z; s[j + 3] = e.s.w;
+      } else {
+#pragma unroll
+        for (int x = j; x < j + 4; ++x) {
+          const float *row = q8_angle_row(rope, at, at_i + x, D) + at_i + x;
+          c[x] = row[0];
+          s[x] = row[D / 2];
+        }
+      }
+    }
+  }
+  const float inv_d = 1.f / (float)D;
+  const int h0 = blockIdx.y * heads, h1 = min(h0 + heads, Hq + Hkv);
+  for (int h = h0; h < h1; h += kHeadsAtOnce) {
+    uint4 lo[kHeadsAtOnce], hi[kHeadsAtOnce];
+    auto place = [&](int j) { return (((size_t)(j < Hq ? b * Hq + j : b * Hkv + j - Hq)) * L + t) * D + at_i; };
+#pragma unroll
+    for (int x = 0; x < kHeadsAtOnce; ++x) {
+      const int j = min(h + x, h1 - 1);
+      const T *p = (j < Hq ? q : k) + place(j);
+      lo[x] = *reinterpret_cast<const uint4 *>(p);
+      hi[x] = *reinterpret_cast<const uint4 *>(p + D / 2);
+    }
+#pragma unroll
+    for (int x = 0; x < kHeadsAtOnce; ++x) {
+      if (h + x >= h1) break;
+      const T *weight = (h + x < Hq ? q_weight : k_weight) + at_i;
+      float u[E], w[E], gu[E], gw[E], y[E], z[E];
+      unpack<T>(lo[x], u);
+      unpack<T>(hi[x], w);
+      unpack<T>(*reinterpret_cast<const uint4 *>(weight), gu);
+      unpack<T>(*reinterpret_cast<const uint4 *>(weight + D / 2), gw);
+      auto squares = [&] {
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < E; ++j) sum = fmaf(u[j], u[j], fmaf(w[j], w[j], sum));
+        if (!there) sum = 0.f;
+        for (int o = 1; o < lanes; o <<= 1) sum += __shfl_xor(sum, o, 64);
+        return sum * inv_d;
+      };
+      const float mean = squares();
+      float r = 1.f / sqrtf(mean + eps);
+      if (__builtin_expect(__any(!(mean < INFINITY)), 0)) {  // (a group's lanes have one sum)
+        const float f = mean < INFINITY ? 1.f : kSmall;
+#pragma unroll
+        for (int j = 0; j < E; ++j) u[j] *= f, w[j] *= f;
+        const float small = squares();
+        r = mean < INFINITY ? r : 1.f / sqrtf(small + eps * kSmall * kSmall);
+      }
+#pragma unroll
+      for (int j = 0; j < E; ++j) {
+#pragma clang fp contract(off)
+        const float a = u[j] * r * gu[j], e = w[j] * r * gw[j];
+        y[j] = rope.table ? q8_turn(a, e, c[j], s[j], true) : a;
+        z[j] = rope.table ? q8_turn(e, a, c[j], s[j], false) : e;
+      }
+      if (!there) continue;
+      T *p = (h + x < Hq ? q_out : k_out) + place(h + x);
+      *reinterpret_cast<uint4 *>(p) = pack<T>(y);
+      *reinterpret_cast<uint4 *>(p + D / 2) = pack<T>(z);
+    }
+  }
+}
+
 }  // namespace
 
 hipError_t ag_launch_rotate(ag_ctx *ctx, hipStream_t s, const void *q, const void *k, ag_dtype dt, int B, int Hq, int Hkv, int L,
@@ -100,5 +188,25 @@ hipError_t ag_launch_rotate(ag_ctx *ctx, hipStream_t s, const void *q, const voi
   else
     AG_LAUNCH(ag_time_kernel(ctx, AG_K_ROTATE), ag_rotate_kernel<float>, grid, dim3(256), 0, s, (const float *)q, (const float *)k,
               (float *)q_out, (float *)k_out, tokens, Hq, Hkv, L, D, heads, rope, ctx->d_err);
+  return hipGetLastError();
+}
+
+hipError_t ag_launch_norm_rotate(ag_ctx *ctx, hipStream_t s, const void *q, const void *k, ag_dtype dt, int B, int Hq, int Hkv, int L,
+                                 int D, const void *q_weight, const void *k_weight, float eps, const ag_rope_dev &rope, void *q_out, void *k_out) {
+  const int tokens = B * L, E = dt == AG_BF16 ? 8 : 4, H = Hq + Hkv;
+  int lanes_log = 0;
+  while ((1 << lanes_log) < D / 2 / E) ++lanes_log;  // at most 64: D <= 512
+  const int64_t wgs = (((int64_t)tokens << lanes_log) + 255) / 256;
+  int heads = 16;  // as for the rotation
+  while (heads > 1 && wgs * ((H + heads - 1) / heads) < 8 * ctx->num_cu) heads /= 2;
+  const dim3 grid((unsigned)wgs, (H + heads - 1) / heads);
+  if (dt == AG_BF16)
+    AG_LAUNCH(ag_time_kernel(ctx, AG_K_NORM_ROTATE), ag_norm_rotate_kernel<uint16_t>, grid, dim3(256), 0, s, (const uint16_t *)q, (const uint16_t *)k,
+              (uint16_t *)q_out, (uint16_t *)k_out, (const uint16_t *)q_weight, (const uint16_t *)k_weight, eps, tokens, Hq, Hkv, L, D, lanes_log,
+              heads, rope, ctx->d_err);
+  else
+    AG_LAUNCH(ag_time_kernel(ctx, AG_K_NORM_ROTATE), ag_norm_rotate_kernel<float>, grid, dim3(256), 0, s, (const float *)q, (const float *)k,
+              (float *)q_out, (float *)k_out, (const float *)q_weight, (const float *)k_weight, eps, tokens, Hq, Hkv, L, D, lanes_log, heads, rope,
+              ctx->d_err);
   return hipGetLastError();
 }
