@@ -379,7 +379,7 @@ ag_status ag_q8_decode_attn(ag_ctx *ctx, void *hip_stream, const void *q, const 
  * ag_q8_tree_attn: node t of query head i (KV head g = i / (Hq/Hkv)) sees the unit's rows as the cache holds them, those nodes above it
  * in its tree with flags[b,g,.] != 0 (flags = NULL: all), and itself; out as in ag_q8_prefill_attn, of which a chain is the case
  * parent[t] = t - 1.  The cache is only read.  q, out [B, Hq, L, D]; k, v [B, Hkv, L, D].  One launch.
- * B * Hkv * (max_blocks + 16) times the number of 128-row tiles of L * (Hq / Hkv) rows must stay below 2^31 - 2^16.
+ * B * Hkv * (max_blocks + 16) times the number of 32-row tiles of L * (Hq / Hkv) rows must stay below 2^31 - 2^16.
  *
  * ag_q8_tree_append: the accepted path joins the cache: of the nodes above last[b] (device int32 [B]; negative: none) and last[b] itself, those
  * with flags[b,g,.] != 0, in order, as ag_q8_append appends them.  A last[b] >= L counts as none (ag_poll_error: AG_EINVAL).  Needs no workspace.
