@@ -25,6 +25,7 @@
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
+typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4;
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
 constexpr int kMostUnits = 8 * 64;  // units up to which every wave goes through the list by itself
 constexpr int kPageBits = 6;   // a page's values are made as large as 2^15 (codes below 2^9)
@@ -51,12 +52,21 @@ struct tree_args {
 __device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32, 64); }
 // x 2^d, d <= 0, in two steps: references of pages of very different sizes lie further apart than a factor can be small
 __device__ __forceinline__ float shrink(float x, float half) { return x * half * half; }
+// Eight values of row r of a group of 32 (as units of 8 values): fragment by fragment, in an order of the rows that keeps the eight pieces of a
+// row that neighbouring lanes write in different banks.
+template <int D> __device__ __forceinline__ int fragment(int group, int step, int half, int r) {
+  const int unit = step * 2 + half;
+  return (group * (D / 8) + unit) * 32 + (r ^ (unit & 7));
+}
 // Where values d .. d + 7 of row r lie in fragments of 32 rows (as units of 8 values): step (d / 64, d / 32 % 2, d / 8 % 2), half d / 16 % 2.
 // (A 16-byte piece of a page, 16 columns, is a half's part of two steps.)
 template <int D> __device__ __forceinline__ int frag_at(int r, int d) {
   const int step = d / 64 * 4 + d / 32 % 2 * 2 + d / 8 % 2;
-  return (((r >> 5) * (D / 16) + step) * 2 + d / 16 % 2) * 32 + (r & 31);
+  return fragment<D>(r >> 5, step, d / 16 % 2, r & 31);
 }
+// Where the 16-byte piece c of a value row lies: rows of D, their pieces in an order that keeps the four rows of a transposing read, and the rows
+// that a wave writes, in different banks.
+template <int D> __device__ __forceinline__ int value_at(int r, int c) { return r * D + (c ^ (D == 128 ? (r & 3) << 2 | (r >> 2 & 3) : (r & 3) << 1 | (r >> 2 & 1))) * 8; }
 // The first of the eight columns that half h has in a step.
 __device__ __forceinline__ int step_col(int step, int h) { return step / 4 * 64 + step / 2 % 2 * 32 + h * 16 + step % 2 * 8; }
 
@@ -383,11 +393,11 @@ __global__ __launch_bounds__(kThreads, 2) void ag_q8_tree_kernel(tree_args a) {
           if (d == 0) s_ek[r] = ek;
           if (odd) atomicOr(reinterpret_cast<unsigned long long *>(&s_odd[r >> 6]), 1ull << (r & 63));
         }
-        // value row r (of 64) of column 32 f + c: step r / 16, half r / 4 % 2, element 4 (r / 8 % 2) + r % 4 (rows that are not there: zeros)
-        const uint32_t w[8] = {rows_in.v[i].lo.x, rows_in.v[i].lo.y, rows_in.v[i].lo.z, rows_in.v[i].lo.w, rows_in.v[i].hi.x, rows_in.v[i].hi.y, rows_in.v[i].hi.z, rows_in.v[i].hi.w};
-        uint16_t *to = s_v + (r >> 6) * S::kTile + (d >> 5) * 2048 + (d & 31) * 8 + ((r >> 4 & 3) * 64 + (r >> 2 & 1) * 32) * 8 + (r >> 3 & 1) * 4 + (r & 3);
-#pragma unroll
-        for (int z = 0; z < 16; ++z) to[z / 8 * (D / 64 * 2048) + z % 8 * 8] = there ? (uint16_t)(w[z / 2] >> (16 * (z & 1))) : (uint16_t)0;
+        // values row by row (rows that are not there: zeros), where the transposing reads find them
+        const uint32_t keep = there ? ~0u : 0u;
+        const uint4 lo = rows_in.v[i].lo, hi = rows_in.v[i].hi;
+        *reinterpret_cast<uint4 *>(s_v + value_at<D>(r, d / 8)) = make_uint4(lo.x & keep, lo.y & keep, lo.z & keep, lo.w & keep);
+        *reinterpret_cast<uint4 *>(s_v + value_at<D>(r, (d + D / 2) / 8)) = make_uint4(hi.x & keep, hi.y & keep, hi.z & keep, hi.w & keep);
       }
     };
     {
@@ -510,7 +520,7 @@ __global__ __launch_bounds__(kThreads, 2) void ag_q8_tree_kernel(tree_args a) {
     q8_f32x16 o[DT];
     float m = kQ8EmptyMax, l = 0.f;
 #pragma unroll
-    for (int i = 0; i < KS; ++i) qx[i] = *reinterpret_cast<const q8_f16x8 *>(s_q + ((rg * KS + i) * 64 + lane) * 8);
+    for (int i = 0; i < KS; ++i) qx[i] = *reinterpret_cast<const q8_f16x8 *>(s_q + fragment<D>(rg, i, h, col) * 8);
     const int eq = s_eq[rg * 32 + col];
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
@@ -696,14 +706,14 @@ __global__ __launch_bounds__(kThreads, 2) void ag_q8_tree_kernel(tree_args a) {
         const uint64_t all = seen(lt), odd = s_odd[which], bits = all & ~odd;
         const uint32_t half_bits = (uint32_t)(bits >> (32 * x));
         if (active && half % KW == KW - 1 - kg && __any(half_bits != 0)) {
-          const uint16_t *kf = s_k + which * S::kTile + x * KS * 512 + lane * 8, *vf = s_v + which * S::kTile + 2 * x * 512 + lane * 8;
+          const uint16_t *kf = s_k + which * S::kTile + x * KS * 512, *vf = s_v + which * S::kTile + x * 32 * D;
           q8_f32x16 s;
 #pragma unroll
           for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
           for (int k = 0; k < KS; ++k)
-            s = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const q8_f16x8 *>(kf + k * 512),
-                                                       *reinterpret_cast<const q8_f16x8 *>(s_q + ((rg * KS + k) * 64 + lane) * 8), s, 0, 0, 0);
+            s = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const q8_f16x8 *>(kf + fragment<D>(0, k, h, col) * 8),
+                                                       *reinterpret_cast<const q8_f16x8 *>(s_q + fragment<D>(rg, k, h, col) * 8), s, 0, 0, 0);
           float mx = -INFINITY;
           const uint32_t w = half_bits >> (4 * h);
 #pragma unroll
@@ -734,7 +744,12 @@ __global__ __launch_bounds__(kThreads, 2) void ag_q8_tree_kernel(tree_args a) {
             const q8_bf16x8 ph = __builtin_bit_cast(q8_bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3])), pl = __builtin_bit_cast(q8_bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) {
-              const q8_bf16x8 v = *reinterpret_cast<const q8_bf16x8 *>(vf + (dt * 4 + i) * 512);
+              // rows 16 i + 4 h + 0..3 and 8 further of this lane's column: lane x of 16 gives the address of row x / 4, columns 4 (x % 4) ...
+              const int r = 4 * h + (lane >> 2 & 3), c = 4 * dt + (lane >> 4 & 1) * 2 + (lane >> 1 & 1);
+              auto read = [&](int row) {
+                return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4 *)(vf + 16 * i * D + value_at<D>(row, c) + (lane & 1) * 4));
+              };
+              const q8_bf16x8 v = __builtin_shufflevector(read(r), read(r + 8), 0, 1, 2, 3, 4, 5, 6, 7);
               o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pl, o[dt], 0, 0, 0);
               o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, ph, o[dt], 0, 0, 0);
             }
@@ -761,7 +776,7 @@ __global__ __launch_bounds__(kThreads, 2) void ag_q8_tree_kernel(tree_args a) {
                 z = q8_turn8<D>(angles, c, y, other);
               }
             }
-            const q8_f16x8 q = *reinterpret_cast<const q8_f16x8 *>(s_q + ((rg * KS + k) * 64 + lane) * 8);
+            const q8_f16x8 q = *reinterpret_cast<const q8_f16x8 *>(s_q + fragment<D>(rg, k, h, col) * 8);
 #pragma unroll
             for (int i = 0; i < 4; ++i) s = fmaf((float)q[i], z.a[i], fmaf((float)q[4 + i], z.b[i], s));
           }
