@@ -31,7 +31,7 @@ constexpr int kMostUnits = 8 * 64;  // units up to which every wave goes through
 constexpr int kPageBits = 6;   // a page's values are made as large as 2^15 (codes below 2^9)
 constexpr int kSpan = 12;      // a page's values are scaled up at most 2^kSpan more than those of the page with the largest ones ...
 constexpr int kLeastExp = -90; // ... and at most 2^90: exact still (codes down to 2^-9, scales to 2^-100), and row sums of 2^18 rows stay in range
-constexpr int kUnitCost = 6;   // what a tile costs beside its pages, in pages
+constexpr int kUnitCost = 10;   // what a tile costs beside its pages, in pages
 constexpr float kLocalBits = 9.f;  // rows that a tree and a tail can have: below 2^9
 constexpr int kWords = kQ8TreeMost / 64;
 
@@ -705,7 +705,7 @@ __global__ __launch_bounds__(kThreads, 2) void ag_q8_tree_kernel(tree_args a) {
         const int own = held + t - lt * kQ8Block;  // the tile's row that is this lane's own node
         const uint64_t all = seen(lt), odd = s_odd[which], bits = all & ~odd;
         const uint32_t half_bits = (uint32_t)(bits >> (32 * x));
-        if (active && half % KW == KW - 1 - kg && __any(half_bits != 0)) {
+        if (active && (KW == 2 ? kg == 0 : half % KW == kg) && __any(half_bits != 0)) {
           const uint16_t *kf = s_k + which * S::kTile + x * KS * 512, *vf = s_v + which * S::kTile + x * 32 * D;
           q8_f32x16 s;
 #pragma unroll

@@ -40,7 +40,8 @@ def expect_capacity(ctx):
     ctx.poll_error()
 
 
-@pytest.mark.parametrize("U,n_pages,blocks,rows", [(1, 1, 1, 64), (4, 9, 3, 64), (6, 5000, 40, 200), (1030, 9000, 5, 130), (3, 12289, 2100, 64 * 2000), (5, 20, 3, 0)])
+@pytest.mark.parametrize("U,n_pages,blocks,rows", [(1, 1, 1, 64), (4, 9, 3, 64), (6, 5000, 40, 200), (1030, 9000, 5, 130), (3, 12289, 2100, 64 * 2000), (5, 20, 3, 0),
+                                                      (1024, 8192, 30, 64 * 3 + 63), (1024, 8193, 30, 64 * 3 + 63), (1025, 3000, 4, 100), (7, 900, 40, 64 * 4), (1024, 700, 3, 64)])
 def test_reserve(U, n_pages, blocks, rows):
     g = gen(U + n_pages)
     pool = Pool(g, n_pages, 64)
