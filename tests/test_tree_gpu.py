@@ -128,6 +128,63 @@ def test_values_of_any_size(D, lens, values):
         assert e.max() <= bar()
 
 
+@pytest.mark.parametrize("D,lens", [(128, [64 * 9 + 5, 64 * 20]), (64, [64 * 5, 64 * 40 + 63])])
+def test_pages_of_different_sizes(D, lens):
+    """Blocks of zeros (their rows count in the row sum), blocks 2^-60 to 2^60 as large as others, keys of different sizes."""
+    g = gen(D + 7)
+    for kind in ("zeros", "small", "large", "mixed", "keys"):
+        ref = cache_of(1, 2, D, lens, 0, g)
+        n = ref.n_pages
+        if kind == "zeros":
+            some_pages = torch.rand(n, generator=g) < 0.5
+            ref.codes[1][some_pages] = 0.0
+            ref.scales[1][some_pages] = 2.0 ** -100
+        elif kind == "keys":
+            size = torch.exp2(torch.randint(-8, 1, (n,), generator=g).float())
+            ref.scales[0] *= size
+        else:
+            lo, hi = {"small": (-60, 1), "large": (0, 61), "mixed": (-60, 61)}[kind]
+            ref.scales[1] *= torch.exp2(torch.randint(lo, hi, (n,), generator=g).float())
+        got, want = tree_both(ref, g, 8, 20, 1, "rand", "mixed")
+        e = row_errors(got, want)
+        print("pages", kind, "%.2e" % e.max().item(), flush=True)
+        assert e.max() <= bar()
+
+
+@pytest.mark.parametrize("size", [2.0 ** -60, 2.0 ** -20, 2.0 ** 20, 2.0 ** 60])
+def test_queries_of_any_size(size):
+    """The scores are the usual ones: the scale makes up for it."""
+    g, D = gen(31), 128
+
+    def touch(q, k, v, f, parent):
+        q *= size
+
+    got, want = tree_both(cache_of(1, 2, D, [100, 300], 0, g), g, 4, 12, 1, "rand", "mixed", scale=D ** -0.5 / size, touch=touch)
+    assert row_errors(got, want).max() <= bar()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_rows_of_the_cache_that_are_not_finite(D):
+    """In the tail (taken one by one) and in pages: columns of a value that is not finite are not finite, everything else is as it should be."""
+    g, H = gen(D + 3), 4
+    ref = cache_of(1, H, D, [64 + 20, 64 + 20, 64 * 2 + 5, 64 * 2 + 5], 0, g)
+    at = R.places(D)
+    ref.tails[1][0][at[1][7, 3]], ref.tails[1][0][at[1][19, 9]] = float("inf"), float("nan")
+    ref.tails[0][1][at[0][11, 2]] = float("nan")                      # a key: every row of the unit
+    ref.codes[1][ref.page[2, 1]][at[1][40, 5]] = float("nan")
+    ref.codes[0][ref.page[3, 0]][at[0][1, 1]] = float("nan")
+    got, want = tree_both(ref, g, H, 10, 0, "rand", "mixed")
+    got = got.cpu()
+    for u in range(H):
+        for t in range(10):
+            a, b = got[0, u, t].double(), want[0, u, t]
+            assert torch.equal(torch.isnan(a), torch.isnan(b)) and torch.equal(a[torch.isinf(b)], b[torch.isinf(b)])
+            fine = torch.isfinite(b)
+            if fine.any():
+                assert (a[fine] - b[fine]).pow(2).mean().sqrt() <= bar() * b[fine].pow(2).mean().sqrt()
+    assert torch.isnan(want[0, 1]).all() and torch.isnan(want[0, 3]).all() and torch.isinf(want[0, 0, 0, 3]) and torch.isnan(want[0, 2, 0, 5])
+
+
 @pytest.mark.parametrize("spread", [3.0, 7.0, 30.0])
 @pytest.mark.parametrize("D,lens", [(128, [0, 700]), (64, [130, 64])])
 def test_sharp_scores(D, lens, spread):
