@@ -309,7 +309,8 @@ ag_status ag_rotate(ag_ctx *ctx, void *hip_stream, const void *q, const void *k,
  *   n_i = (x_i r) w_i,   r = 1 / sqrt(mean_i x_i^2 + eps),   w = q_weight (k_weight)
  * and n is turned as ag_rotate turns it; all in 32 bits, products and sums rounded one by one, one rounding to `dtype` at the end.  rope = NULL: n
  * itself.  q_weight, k_weight [D] in `dtype`; eps >= 2^-100; k, k_out and k_weight may be NULL together (Hkv is then ignored).  Layouts, types,
- * D and alignment (the weights' too) as for ag_rotate; q_out may be q, k_out may be k.  Needs no workspace.
+ * D and alignment (the weights' too) as for ag_rotate; q_out may be q, k_out may be k.  Needs no workspace.  At most 2^32 - 256 threads, of which a
+ * token has as many as D / 2 values have pieces of 16 bytes, rounded up to a power of two.
  */
 ag_status ag_norm_rotate(ag_ctx *ctx, void *hip_stream, const void *q, const void *k, ag_dtype dtype, int B, int Hq, int Hkv, int L,
                          int D, const void *q_weight, const void *k_weight, float eps, const ag_rope *rope, void *q_out, void *k_out);
@@ -413,7 +414,7 @@ ag_status ag_q8_tree_append(ag_ctx *ctx, void *hip_stream, const void *k, const 
  *
  * ag_q8_compact_pages: the pages in use move together: used[0] (device int32) receives their number N, and the i-th page in use of those
  * behind N (in increasing order) moves, with its scales and count, to the i-th free one of those before.  moved (device int32 [n_pages]) receives
- * every page's new number, -1 for free ones.  Of cache only k, v, scales and n_pages count.  Then every cache over the pool needs
+ * every page's new number, -1 for free ones, and is another array than ref.  Of cache only k, v, scales and n_pages count.  Then every cache over the pool needs
  * ag_q8_remap: its table's entries become moved[entry].  Pages that are free afterwards hold anything.
  *
  * ag_q8_pool_workspace_bytes covers all of these on caches of up to B * Hkv units; only ag_q8_reserve and ag_q8_compact_pages need any.

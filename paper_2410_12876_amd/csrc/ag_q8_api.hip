@@ -217,7 +217,11 @@ ag_status ag_norm_rotate(ag_ctx *ctx, void *hip_stream, const void *q, const voi
   AG_REQUIRE(dtype == AG_F32 || dtype == AG_BF16, AG_EINVAL, "ag_norm_rotate: unknown dtype %d", (int)dtype);
   AG_REQUIRE(eps >= 0x1p-100f && isfinite(eps), AG_EINVAL, "ag_norm_rotate: eps must be finite and at least 2^-100");
   AG_REQUIRE(D % 16 == 0 && D <= 512, AG_EUNSUPPORTED, "ag_norm_rotate: D = %d (a multiple of 16, at most 512)", D);
-  AG_REQUIRE(L <= kMaxL && (int64_t)B * L < (1ll << 31) && (int64_t)Hq + Hkv <= 65535, AG_EUNSUPPORTED, "ag_norm_rotate: problem too large");
+  const int piece = dtype == AG_BF16 ? 8 : 4;  // (a token's threads: its pairs' pieces of 16 bytes, rounded up to a power of two; a launch has fewer than 2^32)
+  int64_t threads = (int64_t)B * L;
+  for (int n = 1; n < D / 2 / piece; n *= 2) threads *= 2;
+  AG_REQUIRE(L <= kMaxL && (int64_t)B * L < (1ll << 31) && threads <= (1ll << 32) - 256 && (int64_t)Hq + Hkv <= 65535, AG_EUNSUPPORTED,
+             "ag_norm_rotate: problem too large");
   AG_REQUIRE(aligned({q, k, q_weight, k_weight, q_out, k_out}), AG_EINVAL, "ag_norm_rotate: tensors must be 16-byte aligned");
   ag_rope_dev r;
   ag_status st = check_rope(ctx, "ag_norm_rotate", rope, D, (int64_t)B * L, &r, false);
@@ -339,6 +343,7 @@ ag_status ag_q8_compact_pages(ag_ctx *ctx, void *hip_stream, ag_q8_cache *cache,
   ag_status st = check_pool(ctx, "ag_q8_compact_pages", cache, ref, &c);
   if (st != AG_OK) return st;
   AG_REQUIRE(moved && used, AG_EINVAL, "ag_q8_compact_pages: null pointer");
+  AG_REQUIRE(moved != ref, AG_EINVAL, "ag_q8_compact_pages: moved and ref are one array");
   ws_cursor ws{ctx->ws, ctx->ws_bytes, 0, true};
   const ag_q8_pool_ws w = take_pool(ws, 1, cache->n_pages);
   AG_REQUIRE(ws.ok, AG_EWORKSPACE, "ag_q8_compact_pages: workspace of %zu bytes is too small (need %zu)", ctx->ws_bytes, ws.off);

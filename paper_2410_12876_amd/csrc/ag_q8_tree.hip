@@ -933,8 +933,11 @@ hipError_t launch_rows(ag_ctx *ctx, hipStream_t s, tree_args &a) {
 
 }  // namespace
 
-// (and what rounding up to whole ranges adds)
-int64_t ag_q8_tree_cost(int64_t units, int rows, int max_blocks) { return units * ((int64_t)max_blocks + kUnitCost) * tiles_of(rows, 1) + (1 << 16); }
+// (with what rounding up adds)
+int64_t ag_q8_tree_cost(int64_t units, int rows, int max_blocks) {
+  static_assert(kUnitCost <= 16, "the bound is part of the interface");
+  return units * ((int64_t)max_blocks + 16) * tiles_of(rows, 1) + (1 << 16);
+}
 
 // Two records a workgroup, of as many groups of rows as it may have.
 size_t ag_ws_q8_tree_floats(int num_cu, int rows, int D) {

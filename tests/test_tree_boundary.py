@@ -1,4 +1,5 @@
 """The boundary of the normalised rotation, of trees and of page pools without a GPU: refusals, sizes, and the reference that the GPU tests use."""
+import ctypes as C
 import math
 
 import pytest
@@ -33,6 +34,18 @@ def test_norm_rotate_refusals(lib):  # noqa: F811
                 (q, k, w, w, 1e-6, r, q.float(), k), (q, k, w, w, 1e-6, r, q, k[:, :1].contiguous())):
         with pytest.raises(ValueError):
             call(*bad)
+    ctx.close()
+
+
+def test_norm_rotate_of_more_threads_than_a_launch_has(lib):  # noqa: F811
+    """A token of 512 bf16 values has 32 threads, one of 272 values too; a launch has fewer than 2^32."""
+    ctx, x = ag.Context(device=-1), torch.zeros(512, dtype=BF)
+    raw = lambda B, D: lib.ag_norm_rotate(C.c_void_p(ctx._addr), None, C.c_void_p(x.data_ptr()), None, ag.AG_BF16, B, 1, 0, 1, D, C.c_void_p(x.data_ptr()), None,  # noqa: E731
+                                          C.c_float(1e-6), None, C.c_void_p(x.data_ptr()), None)
+    for D in (512, 272):
+        assert raw((1 << 27) - 8, D) == ag.AG_EHIP
+        assert raw(1 << 27, D) == ag.AG_EUNSUPPORTED
+    assert raw((1 << 31) - 1, 16) == ag.AG_EHIP
     ctx.close()
 
 
@@ -106,6 +119,7 @@ def test_pool_refusals(lib):  # noqa: F811
     expect(ag.AG_EHIP, ag.ag_q8_compact_pages, ctx, a, ref, ref.clone(), used, stream=0)
     expect(ag.AG_EHIP, ag.ag_q8_remap, ctx, a, ref, stream=0)
     expect(ag.AG_EINVAL, ag.ag_q8_reserve, ctx, a, ref, -1, stream=0)
+    expect(ag.AG_EINVAL, ag.ag_q8_compact_pages, ctx, a, ref, ref, used, stream=0)
     for bad in (ref[:5], ref.long()):
         for call in (lambda x: ag.ag_q8_reserve(ctx, a, x, 1, stream=0), lambda x: ag.ag_q8_release(ctx, a, x, which, stream=0),
                      lambda x: ag.ag_q8_fork(ctx, a, par, b, x, stream=0), lambda x: ag.ag_q8_compact_pages(ctx, a, x, ref, used, stream=0),
