@@ -2,18 +2,23 @@
 // and to itself.
 //
 // Query rows of a unit are its nodes' heads, r = t G + head; a wave owns 32 of them, a lane one column: S^T = K q^T, O^T = V^T p^T on
-// v_mfma_f32_32x32x16.  Bound by the pages' bytes while a unit has few rows, beyond by the matrix instructions and the weights between them.
+// v_mfma_f32_32x32x16.  Bound by the pages' bytes while a unit has few rows (32 rows: 0.65 us a page of 16 KiB a CU, 6.5 TB/s; 64: 0.83 us, 5.05 TB/s),
+// beyond by the matrix instructions and the conversions and weights between them (128: 1.30 us, 0.82 PFLOP/s).  A short call is a chain of
+// round trips: 12 nodes over 777 rows 14.8 us; 16 x 31 nodes over 4096 rows 40.5 us, of which the pages take 23, the start 8 and the meetings 7.
 //   * A page goes from memory into the registers as it lies, and there, made f16 (exact, two values an instruction), into the product: its
 //     16-byte pieces are 16 columns of a row (4 x 4 rows of a column) for either half of the wave, in the order in which the query's
 //     (the weights') registers are.  No LDS, no barrier between pages; a page's registers are asked for again as soon as they are used up.
-//   * A workgroup of 8 waves has RW groups of 32 rows and 8 / RW waves for each, which take every so many-th page; their states are added up in LDS at the end.
-//   * Up to as many (unit, tile of RW groups) as there are workgroups: every tile gets workgroups in proportion to its cost, its pages and
-//     kUnitCost; beyond, all tiles are one list end to end, of which a workgroup takes an equal range.  Where several work on a tile they leave their
-//     states as records, and the one that comes last adds them up in order.
-//   * The tail's rows and the nodes are one sequence of rows behind each other, 64 of them a tile in LDS: keys (turned) in f16 times a power of
-//     two for each, values in bf16 and weights as the sum of two bf16, so rows of any size keep 11 and 16 bits.  Nodes that a row may not see are
-//     masked by the bits of its ancestors, which pointers that double in length find in log2(L) steps.  Rows with infinities or NaN are taken
-//     one by one in 32 bits, by those who see them.
+//     (Through LDS, where the groups share one copy: 1.30 against 1.35 us a page then, but with room for fewer local rows 62 against 57 us for
+//     4 x 64 nodes over 13000.)
+//   * A workgroup of 8 waves, one a CU (two of 4 waves: 50 against 46 us for 16 x 31 nodes), has RW groups of 32 rows and 8 / RW waves for each, which
+//     take every so many-th page; their states are added up in LDS at the end.
+//   * Every tile (a unit's RW groups) is cut into pieces by its cost, its pages and kUnitCost; a workgroup takes one piece.  (Equal ranges of all tiles
+//     end to end balance better, but what lives across that loop cost more: 83 against 57 us for 16 x 31 nodes.)  The pieces of a cut tile leave
+//     their states as records, and the one that comes last adds them up in order.
+//   * The tail's rows and the nodes are one sequence of rows behind each other, 128 at a time (two tiles of 64) in LDS: keys (turned) in f16 times
+//     a power of two for each, values in bf16 and weights as the sum of two bf16, so rows of any size keep 11 and 16 bits.  Nodes that a row may not
+//     see are masked by the bits of its ancestors, which pointers that double in length find in log2(L) steps.  Rows with infinities or NaN are
+//     taken one by one in 32 bits, by those who see them.  The waves that leave their pages first, the older ones, take them (42 -> 40.5 us).
 //   * Queries, page values and page weights are f16 times powers of two, 11 bits of each; the weights' reference lies 2^-kQ8TopBits below the largest
 //     of the page that set it and is moved only when weights pass 2^15.  A page's values are as large as f16 holds them unless a page of the
 //     same wave has ones 2^kSpan as large: then less, or the weights of such a page (one of zeros, say) would be too small for f16 and its rows
@@ -31,7 +36,7 @@ constexpr int kMostUnits = 8 * 64;  // units up to which every wave goes through
 constexpr int kPageBits = 6;   // a page's values are made as large as 2^15 (codes below 2^9)
 constexpr int kSpan = 12;      // a page's values are scaled up at most 2^kSpan more than those of the page with the largest ones ...
 constexpr int kLeastExp = -90; // ... and at most 2^90: exact still (codes down to 2^-9, scales to 2^-100), and row sums of 2^18 rows stay in range
-constexpr int kUnitCost = 10;   // what a tile costs beside its pages, in pages
+constexpr int kUnitCost = 10;   // what a tile costs beside its pages, in pages (16 x 31 nodes over 4096 rows 40.4 us, 4 x 64 over 13000 51.0; 6: 41.4, 51.9; 14: 42.0, 51.7)
 constexpr float kLocalBits = 9.f;  // rows that a tree and a tail can have: below 2^9
 constexpr int kWords = kQ8TreeMost / 64;
 
@@ -899,14 +904,18 @@ __global__ __launch_bounds__(kThreads, 2) void ag_q8_tree_kernel(tree_args a) {
   }
 }
 
-// Groups of 32 rows that a workgroup takes: as many as a unit has (up to 4: they share what they load of the pages), but one where even so a wave
-// has at most two pages.
-int row_groups(int num_cu, int units, int rows, int max_blocks) {
-  const int n = (rows + 31) / 32;
-  if (n == 1 || (int64_t)units * n * max_blocks <= 2 * kWaves * num_cu) return 1;
-  return n == 2 ? 2 : 4;
-}
 int tiles_of(int rows, int groups) { return (rows + 32 * groups - 1) / (32 * groups); }
+// Groups of 32 rows that a workgroup takes.  More of them share what they load of the pages, fewer have more waves for each group's pages and local
+// rows, and less to add up.  So as few as leave a tile for every CU at most, while there are few pages to go through: up to 16 a CU one group (4 x 31
+// nodes over 1500 rows, G = 4, 8 heads: 20.3 us with one, 20.8 with two, 24 with four; over 3000 29 / 26 / 28), up to 96 two (over 9000 57 / 39 / 43; 4 x 64
+// nodes over 13000 54 with two, 51 with four).  With more tiles than CUs the rest would wait: 32 x 16 nodes over 100 rows 29 / 16.
+int row_groups(int num_cu, int units, int rows, int max_blocks) {
+  const int n = tiles_of(rows, 1);
+  const int64_t pages = (int64_t)units * n * max_blocks;
+  if (n == 1 || ((int64_t)units * n <= num_cu && pages <= 16 * num_cu)) return 1;
+  if (n == 2 || ((int64_t)units * tiles_of(rows, 2) <= num_cu && pages <= 96 * num_cu)) return 2;
+  return 4;
+}
 
 template <int D, int RW>
 hipError_t launch(ag_ctx *ctx, hipStream_t s, tree_args &a) {

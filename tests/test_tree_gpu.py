@@ -34,9 +34,12 @@ def tree_ctx(c, L, Hq):
     return ag.Context(0, ag.q8_tree_workspace_bytes(c.B, L, Hq, c.Hkv, c.D, c.max_blocks))
 
 
-def cache_of(B, H, D, lens, room, g, values=0):
+def cache_of(B, H, D, lens, room, g, values=0, width=0):
+    """width: the table has so many columns, those behind the pages empty (a call chooses its tiles by the table, not by the lengths)."""
     blocks = (max(lens) + room) // 64 + 1
     c = R.Cache(B, H, D, B * H * blocks + 2, blocks, g, lens)
+    if width > blocks:
+        c.page, c.max_blocks = torch.cat([c.page, torch.full((B * H, width - blocks), -1, dtype=torch.int32)], 1), width
     c.scales[1] *= 2.0 ** values
     c.tails[1] *= 2.0 ** values
     return c
@@ -128,12 +131,30 @@ def test_values_of_any_size(D, lens, values):
         assert e.max() <= bar()
 
 
+# Widths of a table with which a tile has one, two and four groups of 32 rows, where the rows are that many.
+WIDTHS = [0, 1000, 5000]
+
+
+@pytest.mark.parametrize("a_cu", [60, 120])
+@pytest.mark.parametrize("B,Hq,H,D,L,lens,axes,kind,tree", [
+    (1, 16, 2, 64, 64, [64, 1500], 3, "rand", "mixed"), (1, 4, 2, 128, 33, [3000, 100], 1, "rand", "star"), (1, 4, 4, 128, 200, [0, 65, 128, 777], 1, "none", "chain"),
+    (2, 16, 2, 128, 12, [0, 3, 62, 2000], 3, "rand", "mixed"), (1, 8, 1, 128, 256, [700], 1, "rand", "mixed"), (1, 2, 2, 64, 97, [63, 64 * 70], 0, None, "roots")])
+def test_tree_in_larger_tiles(B, Hq, H, D, L, lens, axes, kind, tree, a_cu):
+    g, tiles = gen(L + D + a_cu), (L * Hq // H + 31) // 32
+    ref = cache_of(B, H, D, lens, 0, g, width=a_cu * 256 // (B * H * tiles) + 1)
+    got, want = tree_both(ref, g, Hq, L, axes, kind, tree)
+    e = row_errors(got, want)
+    print("tree", B, Hq, H, D, L, lens, a_cu, "%.2e" % e.max().item(), flush=True)
+    assert e.max() <= bar()
+
+
+@pytest.mark.parametrize("width", WIDTHS)
 @pytest.mark.parametrize("D,lens", [(128, [64 * 9 + 5, 64 * 20]), (64, [64 * 5, 64 * 40 + 63])])
-def test_pages_of_different_sizes(D, lens):
+def test_pages_of_different_sizes(D, lens, width):
     """Blocks of zeros (their rows count in the row sum), blocks 2^-60 to 2^60 as large as others, keys of different sizes."""
     g = gen(D + 7)
     for kind in ("zeros", "small", "large", "mixed", "keys"):
-        ref = cache_of(1, 2, D, lens, 0, g)
+        ref = cache_of(1, 2, D, lens, 0, g, width=width)
         n = ref.n_pages
         if kind == "zeros":
             some_pages = torch.rand(n, generator=g) < 0.5
@@ -163,20 +184,21 @@ def test_queries_of_any_size(size):
     assert row_errors(got, want).max() <= bar()
 
 
+@pytest.mark.parametrize("L,width", [(10, 0)] + [(70, w) for w in WIDTHS])
 @pytest.mark.parametrize("D", [64, 128])
-def test_rows_of_the_cache_that_are_not_finite(D):
+def test_rows_of_the_cache_that_are_not_finite(D, L, width):
     """In the tail (taken one by one) and in pages: columns of a value that is not finite are not finite, everything else is as it should be."""
     g, H = gen(D + 3), 4
-    ref = cache_of(1, H, D, [64 + 20, 64 + 20, 64 * 2 + 5, 64 * 2 + 5], 0, g)
+    ref = cache_of(1, H, D, [64 + 20, 64 + 20, 64 * 2 + 5, 64 * 2 + 5], 0, g, width=width)
     at = R.places(D)
     ref.tails[1][0][at[1][7, 3]], ref.tails[1][0][at[1][19, 9]] = float("inf"), float("nan")
     ref.tails[0][1][at[0][11, 2]] = float("nan")                      # a key: every row of the unit
     ref.codes[1][ref.page[2, 1]][at[1][40, 5]] = float("nan")
     ref.codes[0][ref.page[3, 0]][at[0][1, 1]] = float("nan")
-    got, want = tree_both(ref, g, H, 10, 0, "rand", "mixed")
+    got, want = tree_both(ref, g, H, L, 0, "rand", "mixed")
     got = got.cpu()
     for u in range(H):
-        for t in range(10):
+        for t in range(L):
             a, b = got[0, u, t].double(), want[0, u, t]
             assert torch.equal(torch.isnan(a), torch.isnan(b)) and torch.equal(a[torch.isinf(b)], b[torch.isinf(b)])
             fine = torch.isfinite(b)
@@ -186,10 +208,11 @@ def test_rows_of_the_cache_that_are_not_finite(D):
 
 
 @pytest.mark.parametrize("spread", [3.0, 7.0, 30.0])
+@pytest.mark.parametrize("width", WIDTHS)
 @pytest.mark.parametrize("D,lens", [(128, [0, 700]), (64, [130, 64])])
-def test_sharp_scores(D, lens, spread):
+def test_sharp_scores(D, lens, spread, width):
     g = gen(int(spread) + D)
-    got, want = tree_both(cache_of(1, 2, D, lens, 0, g), g, 8, 50, 1, "rand", "mixed", scale=spread * D ** -0.5)
+    got, want = tree_both(cache_of(1, 2, D, lens, 0, g, width=width), g, 8, 50, 1, "rand", "mixed", scale=spread * D ** -0.5)
     e = row_errors(got, want)
     print("spread", spread, "%.2e mean %.2e" % (e.max().item(), e.mean().item()), flush=True)
     assert e.max() <= bar(spread)
@@ -216,12 +239,12 @@ def test_many_small_weights():
 
 
 @pytest.mark.parametrize("D", [64, 128])
-@pytest.mark.parametrize("length", [0, 30, 100])
-def test_what_a_node_does_not_see_does_not_reach_it(D, length):
+@pytest.mark.parametrize("length,width", [(0, 0), (30, 0), (100, 0), (30, 1000), (100, 5000)])
+def test_what_a_node_does_not_see_does_not_reach_it(D, length, width):
     """Infinities and NaN in keys and values of nodes, and in rows of the tail that are not there: only those below them see them, and the rest
     has the bits of a clean run."""
     g, L, H, Hq = gen(D + length), 70, 2, 4
-    ref = cache_of(1, H, D, [length] * H, 0, g)
+    ref = cache_of(1, H, D, [length] * H, 0, g, width=width)
     parent = T.random_tree(g, 1, L)
     q, k, v, f = some(g, 1, Hq, L, D), some(g, 1, H, L, D), some(g, 1, H, L, D), flags_of(g, "rand", 1, H, L)
     ctx = tree_ctx(ref, L, Hq)
