@@ -6,7 +6,7 @@
 //     copy, 1024 units 10 us, a small one the chain parent -> length -> table -> count, 3.5 us) and counts the entries.
 //   * Who gets which page needs the free pages' ranks.  ag_q8_list_kernel lists, for every 4096 pages, those in use and then the free ones, and counts; the
 //     second launch finds the chunk of a rank by a search over the counts' prefix sums.  (Taking both from the counts themselves would make
-//     one launch read what another one of its workgroups changes.)
+//     one launch read what another one of its workgroups changes.  For small pools there is a launch that does not.)
 //   * ag_q8_move_kernel: source i is the i-th page in use behind N, destination i the i-th free page before it, so no page is both.  Bound by memory:
 //     5600 pages (184 MB) 29 us.
 #include <algorithm>
@@ -254,6 +254,23 @@ __global__ __launch_bounds__(kThreads) void ag_q8_release_kernel(ag_q8_dev c, in
   if (threadIdx.x == 0) c.len[u] = 0;
 }
 
+// A workgroup copies page p's codes to page `to`.
+template <int D> __device__ __forceinline__ void copy_page(const ag_q8_dev &c, size_t p, size_t to) {
+  constexpr int P = kQ8Block * D / 16 / kThreads;  // 16-byte pieces of a page per thread
+  const int tid = threadIdx.x;
+  q8_u32x4 a[P], b[P];
+  const q8_u32x4 *pk = reinterpret_cast<const q8_u32x4 *>(c.k + p * kQ8Block * D) + tid, *pv = reinterpret_cast<const q8_u32x4 *>(c.v + p * kQ8Block * D) + tid;
+#pragma unroll
+  for (int i = 0; i < P; ++i) a[i] = pk[i * kThreads];
+#pragma unroll
+  for (int i = 0; i < P; ++i) b[i] = pv[i * kThreads];
+  q8_u32x4 *tk = reinterpret_cast<q8_u32x4 *>(c.k + to * kQ8Block * D) + tid, *tv = reinterpret_cast<q8_u32x4 *>(c.v + to * kQ8Block * D) + tid;
+#pragma unroll
+  for (int i = 0; i < P; ++i) tk[i * kThreads] = a[i];
+#pragma unroll
+  for (int i = 0; i < P; ++i) tv[i * kThreads] = b[i];
+}
+
 // Every workgroup takes every n-th of the pages that move, and of the pages whose new number is to be written down.
 template <int D>
 __global__ __launch_bounds__(kThreads) void ag_q8_move_kernel(ag_q8_dev c, int32_t *ref, int32_t *moved, int32_t *used, int chunks, ag_q8_pool_ws w) {
@@ -292,20 +309,50 @@ __global__ __launch_bounds__(kThreads) void ag_q8_move_kernel(ag_q8_dev c, int32
       c.v_scale[to] = c.v_scale[p];
     }
   }
-  constexpr int P = kQ8Block * D / 16 / kThreads;  // 16-byte pieces of a page per thread
-  for (int k = blockIdx.x; k < holes; k += gridDim.x) {
-    const size_t p = used_page(w, s_pre, chunks, N - holes + k), to = free_page(w, s_pre, chunks, c.n_pages, k);
-    q8_u32x4 a[P], b[P];
-    const q8_u32x4 *pk = reinterpret_cast<const q8_u32x4 *>(c.k + p * kQ8Block * D) + tid, *pv = reinterpret_cast<const q8_u32x4 *>(c.v + p * kQ8Block * D) + tid;
+  for (int k = blockIdx.x; k < holes; k += gridDim.x)
+    copy_page<D>(c, used_page(w, s_pre, chunks, N - holes + k), free_page(w, s_pre, chunks, c.n_pages, k));
+}
+
+// The same in one launch for a small pool: every workgroup finds the pages that move by itself, from counts that nobody writes before all have
+// read them: the workgroup that comes last writes the new ones.  500 pages, half in use, 7.5 us (in two launches 11.5), 2000 10.5 (13); 4000 16.5 (14).  More
+// workgroups copy faster but arrive one after the other: 512 of them 8.7 us and 14.4.
+constexpr int kSmallMove = 2048, kSmallMoveWgs = 64;
+template <int D>
+__global__ __launch_bounds__(kThreads) void ag_q8_move_small_kernel(ag_q8_dev c, int32_t *ref, int32_t *moved, int32_t *used, int32_t *ticket) {
+  constexpr int T = kSmallMove / kThreads, WAVES = kThreads / 64;
+  __shared__ uint16_t s_from[kSmallMove / 2], s_to[kSmallMove / 2];
+  __shared__ int32_t sums[WAVES], s_last;
+  const int tid = threadIdx.x, per = (c.n_pages + kThreads - 1) / kThreads;  // a thread has `per` pages behind each other
+  const int p0 = tid * per, p1 = min(c.n_pages, p0 + per);
+  uint32_t in_use = 0;
 #pragma unroll
-    for (int i = 0; i < P; ++i) a[i] = pk[i * kThreads];
-#pragma unroll
-    for (int i = 0; i < P; ++i) b[i] = pv[i * kThreads];
-    q8_u32x4 *tk = reinterpret_cast<q8_u32x4 *>(c.k + to * kQ8Block * D) + tid, *tv = reinterpret_cast<q8_u32x4 *>(c.v + to * kQ8Block * D) + tid;
-#pragma unroll
-    for (int i = 0; i < P; ++i) tk[i * kThreads] = a[i];
-#pragma unroll
-    for (int i = 0; i < P; ++i) tv[i * kThreads] = b[i];
+  for (int i = 0; i < T; ++i)
+    if (p0 + i < p1 && ref[p0 + i] != 0) in_use |= 1u << i;
+  int N, holes, at = wg_prefix<WAVES>(__popc(in_use), N, sums);
+  const int below = max(0, min(p1, N) - p0);  // pages of the thread before N
+  const uint32_t there = p1 > p0 ? (1u << (p1 - p0)) - 1 : 0, ahead = (1u << below) - 1;
+  uint32_t to = ~in_use & there & ahead, from = in_use & ~ahead;
+  int k_to = wg_prefix<WAVES>(__popc(to), holes, sums), unused, k_from = wg_prefix<WAVES>(__popc(from), unused, sums);
+  for (; to; to &= to - 1) s_to[k_to++] = (uint16_t)(p0 + __builtin_ctz(to));
+  for (; from; from &= from - 1) s_from[k_from++] = (uint16_t)(p0 + __builtin_ctz(from));
+  __syncthreads();
+  for (int k = blockIdx.x; k < holes; k += gridDim.x) copy_page<D>(c, s_from[k], s_to[k]);
+  if (tid == 0) s_last = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
+  __syncthreads();
+  if (!s_last) return;
+  if (tid == 0) {
+    ticket[0] = 0;
+    used[0] = N;
+  }
+  for (int i = 0; p0 + i < p1; ++i)
+    if (p0 + i < N || !(in_use >> i & 1)) moved[p0 + i] = in_use >> i & 1 ? p0 + i : -1;
+  for (int k = tid; k < holes; k += kThreads) {
+    const int a = s_from[k], b = s_to[k];
+    moved[a] = b;
+    ref[b] = ref[a];
+    ref[a] = 0;
+    c.k_scale[b] = c.k_scale[a];
+    c.v_scale[b] = c.v_scale[a];
   }
 }
 
@@ -354,6 +401,12 @@ hipError_t ag_launch_q8_release(ag_ctx *ctx, hipStream_t s, int B, int Hkv, cons
 
 hipError_t ag_launch_q8_compact_pages(ag_ctx *ctx, hipStream_t s, const ag_q8_dev &c, int D, int32_t *ref, int32_t *moved, int32_t *used,
                                       const ag_q8_pool_ws &w) {
+  if (c.n_pages <= kSmallMove) {
+    const dim3 wgs(std::max(1, std::min(c.n_pages / 2, kSmallMoveWgs)));
+    if (D == 128) AG_LAUNCH(ag_time_kernel(ctx, AG_K_Q8_PAGES), ag_q8_move_small_kernel<128>, wgs, dim3(kThreads), 0, s, c, ref, moved, used, ctx->decode_tickets);
+    else AG_LAUNCH(ag_time_kernel(ctx, AG_K_Q8_PAGES), ag_q8_move_small_kernel<64>, wgs, dim3(kThreads), 0, s, c, ref, moved, used, ctx->decode_tickets);
+    return hipGetLastError();
+  }
   const hipError_t e = launch_list(ctx, s, c, nullptr, ref, 0, 0, w);
   if (e != hipSuccess) return e;
   const int chunks = ag_q8_page_chunks(c.n_pages), grid = std::min(c.n_pages, 8 * ctx->num_cu);

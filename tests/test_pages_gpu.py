@@ -114,7 +114,8 @@ def test_fork(D, B, B2, H, blocks, more):
 
 
 @pytest.mark.parametrize("D", [64, 128])
-@pytest.mark.parametrize("n_pages,used", [(1, 0.0), (1, 1.0), (70, 0.5), (4096, 0.3), (4097, 0.97), (9000, 0.02), (13000, 0.6), (500, 0.0), (500, 1.0)])
+@pytest.mark.parametrize("n_pages,used", [(1, 0.0), (1, 1.0), (70, 0.5), (4096, 0.3), (4097, 0.97), (9000, 0.02), (13000, 0.6), (500, 0.0), (500, 1.0),
+                                          (2, 0.5), (3, 0.4), (255, 0.9), (257, 0.1), (600, 0.5), (2047, 0.95), (2048, 0.5), (2049, 0.4)])
 def test_compact(D, n_pages, used):
     g = gen(n_pages + D)
     pool = Pool(g, n_pages, D)
@@ -135,6 +136,10 @@ def test_compact(D, n_pages, used):
         assert torch.equal(x.cpu()[want[is_used].long()], y.cpu()[is_used])
     inside = (table >= 0) & (table < n_pages)
     assert torch.equal(c.page.cpu(), torch.where(inside, want[table.clamp(0, n_pages - 1).long()], table))
+    count.fill_(-1)
+    ag.ag_q8_compact_pages(ctx, c, pool.ref, moved, count)  # now they are together
+    at = torch.arange(n_pages)
+    assert int(count) == n and torch.equal(moved.cpu().long(), torch.where(at < n, at, -1)) and torch.equal(pool.ref.cpu(), new)
     ctx.poll_error()
 
 
