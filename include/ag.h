@@ -414,7 +414,7 @@ ag_status ag_q8_tree_append(ag_ctx *ctx, void *hip_stream, const void *k, const 
  *
  * ag_q8_compact_pages: the pages in use move together: used[0] (device int32) receives their number N, and the i-th page in use of those
  * behind N (in increasing order) moves, with its scales and count, to the i-th free one of those before.  moved (device int32 [n_pages]) receives
- * every page's new number, -1 for free ones, and is another array than ref.  Of cache only k, v, scales and n_pages count.  Then every cache over the pool needs
+ * every page's new number, -1 for free ones; ref, moved and used are three arrays.  Of cache only k, v, scales and n_pages count.  Then every cache over the pool needs
  * ag_q8_remap: its table's entries become moved[entry].  Pages that are free afterwards hold anything.
  *
  * ag_q8_pool_workspace_bytes covers all of these on caches of up to B * Hkv units; only ag_q8_reserve and ag_q8_compact_pages need any.

@@ -343,7 +343,7 @@ ag_status ag_q8_compact_pages(ag_ctx *ctx, void *hip_stream, ag_q8_cache *cache,
   ag_status st = check_pool(ctx, "ag_q8_compact_pages", cache, ref, &c);
   if (st != AG_OK) return st;
   AG_REQUIRE(moved && used, AG_EINVAL, "ag_q8_compact_pages: null pointer");
-  AG_REQUIRE(moved != ref, AG_EINVAL, "ag_q8_compact_pages: moved and ref are one array");
+  AG_REQUIRE(moved != ref && used != ref && used != moved, AG_EINVAL, "ag_q8_compact_pages: ref, moved and used share an address");
   ws_cursor ws{ctx->ws, ctx->ws_bytes, 0, true};
   const ag_q8_pool_ws w = take_pool(ws, 1, cache->n_pages);
   AG_REQUIRE(ws.ok, AG_EWORKSPACE, "ag_q8_compact_pages: workspace of %zu bytes is too small (need %zu)", ctx->ws_bytes, ws.off);

@@ -119,7 +119,9 @@ def test_pool_refusals(lib):  # noqa: F811
     expect(ag.AG_EHIP, ag.ag_q8_compact_pages, ctx, a, ref, ref.clone(), used, stream=0)
     expect(ag.AG_EHIP, ag.ag_q8_remap, ctx, a, ref, stream=0)
     expect(ag.AG_EINVAL, ag.ag_q8_reserve, ctx, a, ref, -1, stream=0)
-    expect(ag.AG_EINVAL, ag.ag_q8_compact_pages, ctx, a, ref, ref, used, stream=0)
+    moved = ref.clone()
+    for bad in ((ref, ref, used), (ref, moved, ref[:1]), (ref, moved, moved[:1])):
+        expect(ag.AG_EINVAL, ag.ag_q8_compact_pages, ctx, a, *bad, stream=0)
     for bad in (ref[:5], ref.long()):
         for call in (lambda x: ag.ag_q8_reserve(ctx, a, x, 1, stream=0), lambda x: ag.ag_q8_release(ctx, a, x, which, stream=0),
                      lambda x: ag.ag_q8_fork(ctx, a, par, b, x, stream=0), lambda x: ag.ag_q8_compact_pages(ctx, a, x, ref, used, stream=0),
