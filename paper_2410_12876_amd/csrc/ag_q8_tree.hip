@@ -19,10 +19,9 @@
 //     a power of two for each, values in bf16 and weights as the sum of two bf16, so rows of any size keep 11 and 16 bits.  Nodes that a row may not
 //     see are masked by the bits of its ancestors, which pointers that double in length find in log2(L) steps.  Rows with infinities or NaN are
 //     taken one by one in 32 bits, by those who see them.  The waves that leave their pages first, the older ones, take them (42 -> 40.5 us).
-//   * Queries, page values and page weights are f16 times powers of two, 11 bits of each; the weights' reference lies 2^-kQ8TopBits below the largest
-//     of the page that set it and is moved only when weights pass 2^15.  A page's values are as large as f16 holds them unless a page of the
-//     same wave has ones 2^kSpan as large: then less, or the weights of such a page (one of zeros, say) would be too small for f16 and its rows
-//     missing from the row sum.
+//   * Queries, page values and page weights are f16 times powers of two: 11 bits of a query and of a weight, all of a value's 4.  The weights'
+//     reference lies 2^-kQ8TopBits below the largest of the page that set it and is moved only when weights pass 2^15.  Pages of far smaller values
+//     than others add to the row sum in 32 bits (kQ8Span): 32 more exponentials a lane, in such pages alone.
 #include <algorithm>
 
 #include "ag_q8.h"
@@ -34,8 +33,6 @@ typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4;
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
 constexpr int kMostUnits = 8 * 64;  // units up to which every wave goes through the list by itself
 constexpr int kPageBits = 6;   // a page's values are made as large as 2^15 (codes below 2^9)
-constexpr int kSpan = 12;      // a page's values are scaled up at most 2^kSpan more than those of the page with the largest ones ...
-constexpr int kLeastExp = -90; // ... and at most 2^90: exact still (codes down to 2^-9, scales to 2^-100), and row sums of 2^18 rows stay in range
 constexpr int kUnitCost = 10;   // what a tile costs beside its pages, in pages (16 x 31 nodes over 4096 rows 40.4 us, 4 x 64 over 13000 51.0; 6: 41.4, 51.9; 14: 42.0, 51.7)
 constexpr float kLocalBits = 9.f;  // rows that a tree and a tail can have: below 2^9
 constexpr int kWords = kQ8TreeMost / 64;
@@ -273,7 +270,7 @@ __global__ __launch_bounds__(kThreads, 2) void ag_q8_tree_kernel(tree_args a) {
     const uint16_t *K = a.k + (size_t)u * a.L * D, *V = a.v + (size_t)u * a.L * D;
 
     // ---- a wave's pages: lane x holds the number and the exponents of its page x, of at most 64 at a time ----
-    int ids = -1, ek_v = 0, ev_v = 0, ev_least = kLeastExp;
+    int ids = -1, ek_v = 0, ev_v = 0;
     const int i0 = p0 + kg;
     auto numbers = [&](int first) {
       const int i = first + lane * KW;
@@ -285,12 +282,6 @@ __global__ __launch_bounds__(kThreads, 2) void ag_q8_tree_kernel(tree_args a) {
       ek_v = (int)(__float_as_uint(a.c.k_scale[id]) >> 23) - 127;
       ev_v = (int)(__float_as_uint(a.c.v_scale[id]) >> 23) - 127 - kPageBits;
       ids = ok ? ids : -1;
-    };
-    auto largest_exponent = [&] {
-      int top = ids >= 0 ? ev_v : -255;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) top = max(top, __shfl_xor(top, o, 64));
-      ev_least = max(ev_least, __builtin_amdgcn_readfirstlane(top) - kSpan);
     };
     if (active && i0 < p1) numbers(i0);
 
@@ -517,7 +508,6 @@ __global__ __launch_bounds__(kThreads, 2) void ag_q8_tree_kernel(tree_args a) {
         }
       }
       barrier();
-      if (active && i0 < p1) largest_exponent();
     }
 
     // ---- the pages ----
@@ -533,6 +523,7 @@ __global__ __launch_bounds__(kThreads, 2) void ag_q8_tree_kernel(tree_args a) {
       for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
     if (active && i0 < p1) {
       bool fresh = true;
+      int ev_top = kQ8PageMinExp;  // the largest ev so far
       q8_u32x4 bk[2][KC][2], bv[DT][2];
       const int k_lane = (col >> 4) * KC * 1024 + h * 256 + (col & 15) * 16, v_lane = (col >> 4) * 1024 + h * 256 + (col & 15) * 16;
       constexpr int kAux = RW == 1 ? 2 : 0;  // (pages that other waves do not read too: non-temporal)
@@ -575,8 +566,10 @@ __global__ __launch_bounds__(kThreads, 2) void ag_q8_tree_kernel(tree_args a) {
           const bool more = x + 1 < n;
           // s[i]: row 32 y + 8 (i / 4) + 4 h + i % 4 of the page.  The state is kept relative to m, the largest score plus its page's
           // exponent ev of V less kQ8TopBits: weights are 2^(score + ev - m) in f16, values v 2^-ev, the page's part of the row sum 2^-ev the sum
-          // of its weights as the product takes them.
-          const int e = __builtin_amdgcn_readlane(ev_v, x), ev = max(ev_least, e);
+          // of its weights as the product takes them (`apart`: the sum of 2^(score - m)).
+          const int e = __builtin_amdgcn_readlane(ev_v, x), ev = max(kQ8PageMinExp, e);
+          ev_top = max(ev_top, ev);
+          const bool apart = ev <= ev_top - kQ8Span;
           const float f = q8_unscale(a.qscale, eq + __builtin_amdgcn_readlane(ek_v, x)), scale = q8_pow2(e + kPageBits - ev);
           q8_f32x16 s[2];
           uint32_t p[2][8];
@@ -616,6 +609,13 @@ __global__ __launch_bounds__(kThreads, 2) void ag_q8_tree_kernel(tree_args a) {
             for (int dt = 0; dt < DT; ++dt) o[dt] = o[dt] * alpha * alpha;
             m = m_new;
           };
+          auto row_sum = [&](int y) {
+            if (!apart) return ldexpf(sum, -ev);
+            float w = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) w += __builtin_amdgcn_exp2f(fmaf(s[y][i], f, -m));
+            return w;
+          };
           auto values = [&](int y) {
 #pragma unroll
             for (int i = 2 * y; i < 2 * y + 2; ++i) {
@@ -636,14 +636,14 @@ __global__ __launch_bounds__(kThreads, 2) void ag_q8_tree_kernel(tree_args a) {
             raise(0, false);
             weigh(0);
           }
-          l += ldexpf(sum, -ev);
+          l += row_sum(0);
           values(0);
           weigh(1);
           if (__any(!(sum <= 32768.f))) {
             raise(1, false);
             weigh(1);
           }
-          l += ldexpf(sum, -ev);
+          l += row_sum(1);
           values(1);
           if (more) load_v(x + 1);
         }
@@ -651,7 +651,6 @@ __global__ __launch_bounds__(kThreads, 2) void ag_q8_tree_kernel(tree_args a) {
         if (first_page >= p1) break;
         numbers(first_page);
         exponents();
-        largest_exponent();
       }
     }
 
