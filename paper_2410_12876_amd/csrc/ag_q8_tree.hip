@@ -609,12 +609,10 @@ __global__ __launch_bounds__(kThreads, 2) void ag_q8_tree_kernel(tree_args a) {
             for (int dt = 0; dt < DT; ++dt) o[dt] = o[dt] * alpha * alpha;
             m = m_new;
           };
-          auto row_sum = [&](int y) {
-            if (!apart) return ldexpf(sum, -ev);
-            float w = 0.f;
+          auto sum_apart = [&](int y) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) w += __builtin_amdgcn_exp2f(fmaf(s[y][i], f, -m));
-            return w;
+            for (int i = 0; i < 16; ++i) l += __builtin_amdgcn_exp2f(fmaf(s[y][i], f, -m));
+            sum = 0.f;
           };
           auto values = [&](int y) {
 #pragma unroll
@@ -632,18 +630,20 @@ __global__ __launch_bounds__(kThreads, 2) void ag_q8_tree_kernel(tree_args a) {
           scores(1);
           weigh(0);
           if (more) load_k(x + 1);
-          if (__any(!(sum <= 32768.f))) {
+          if (apart || __any(!(sum <= 32768.f))) {
             raise(0, false);
             weigh(0);
+            if (apart) sum_apart(0);
           }
-          l += row_sum(0);
+          l += ldexpf(sum, -ev);
           values(0);
           weigh(1);
-          if (__any(!(sum <= 32768.f))) {
+          if (apart || __any(!(sum <= 32768.f))) {
             raise(1, false);
             weigh(1);
+            if (apart) sum_apart(1);
           }
-          l += row_sum(1);
+          l += ldexpf(sum, -ev);
           values(1);
           if (more) load_v(x + 1);
         }
