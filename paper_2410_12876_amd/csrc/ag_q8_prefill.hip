@@ -21,7 +21,7 @@
 //   * Weights are f16 too, relative to a reference that lies 2^-8 below the largest (score plus exponent) of the tile that set it: down to
 //     2^-22 of that they keep 11 bits, down to 2^-33 some.  The row sum adds up the rounded ones, so their rounding cancels where many are
 //     alike.  (Against the largest itself and with the unrounded sum, 300000 rows at 2^-25.5 of it put a row off by 1.5e-2 of its size, now by 2.4e-3,
-//     which the store's rounding gives.)
+//     which the store's rounding gives.)  Tiles of far smaller values than others add to the row sum in 32 bits (kQ8Span).
 //   * No maximum is taken in the common case: weights are formed against the reference as it stands, and only if their sum passes 2^15 is
 //     it moved.  The first tile always sets it.
 //   * Few items and long caches: the tiles of an item are cut into up to n_split pieces, whose states a second kernel adds up.
@@ -80,6 +80,9 @@ __device__ __forceinline__ pf_cut cut_of(const pf_args &a, const ag_q8_meta &m, 
 }
 
 __device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32, 64); }
+// 2^(d / 2), d <= 0: what is to shrink by 2^d is multiplied by it twice (references of tiles of very different sizes lie further apart than
+// a factor can be small).
+__device__ __forceinline__ float half_way(float d) { return __builtin_amdgcn_exp2f(0.5f * d); }
 
 template <int D, int G>
 __global__ __launch_bounds__(256, 2) void ag_q8_prefill_kernel(pf_args a) {
@@ -139,6 +142,7 @@ __global__ __launch_bounds__(256, 2) void ag_q8_prefill_kernel(pf_args a) {
     for (int ks = 0; ks < KS; ++ks) qx[ks] = y[ks].f16(inv);
   }
   float m = kQ8EmptyMax, l = 0.f;
+  int ev_top = kQ8PageMinExp;  // the largest exponent that a reference of this wave's rows has been set with
   const bool alone = piece == 0 && (!kept || sole);  // an evicted token sees itself, and so does a kept one that sees nothing else
   q8_f32x16 o[DT];
 #pragma unroll
@@ -166,7 +170,8 @@ __global__ __launch_bounds__(256, 2) void ag_q8_prefill_kernel(pf_args a) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(o[dt][i]) < INFINITY ? fabsf(o[dt][i]) : 0.f);
     top = fmaxf(top, other_half(top));
-    int e = max(kQ8TileMinExp, max(1, (int)(__float_as_uint(top) >> 23)) - 127 - kQ8TileTop) - kQ8TopBits;
+    int e = max(kQ8PageMinExp, max(1, (int)(__float_as_uint(top) >> 23)) - 127 - kQ8TileTop) - kQ8TopBits;
+    ev_top = max(ev_top, e + kQ8TopBits);
     // seeing nothing else its weight is 1 whatever its score is; a score that overflowed to -infinity counts as the least number
     if (sole) s = 0.f, e = 0;
     m = (s < kQ8EmptyMax ? kQ8EmptyMax : s) + (float)e;
@@ -175,15 +180,17 @@ __global__ __launch_bounds__(256, 2) void ag_q8_prefill_kernel(pf_args a) {
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) o[dt] *= scale;
   }
-  // rows that every row of the wave sees, and that one of them sees
+  // rows that every row of the wave sees, and that one of them sees; ev_top over the wave
   int see_all = bound, see_one = bound;
 #pragma unroll
   for (int x = 16; x > 0; x >>= 1) {
     see_all = min(see_all, __shfl_xor(see_all, x, 64));
     see_one = max(see_one, __shfl_xor(see_one, x, 64));
+    ev_top = max(ev_top, __shfl_xor(ev_top, x, 64));
   }
   see_all = __builtin_amdgcn_readfirstlane(see_all);
   see_one = __builtin_amdgcn_readfirstlane(see_one);
+  ev_top = __builtin_amdgcn_readfirstlane(ev_top);
 
   const int32_t *page = a.c.page + (size_t)u * a.c.max_blocks;
   const uint16_t *tiles = a.tiles + (size_t)u * a.n_blk * 2 * HALF;
@@ -254,7 +261,7 @@ __global__ __launch_bounds__(256, 2) void ag_q8_prefill_kernel(pf_args a) {
     }
     if (D == 128 || tid < 128) {
       const int e = __builtin_amdgcn_readlane(w_ev, t - w_first);
-      const float scale = q8_pow2(e + kPageBits - max(kQ8TileMinExp, e));
+      const float scale = q8_pow2(e + kPageBits - max(kQ8PageMinExp, e));
       const uint32_t lo[4] = {rv[0].x, rv[0].y, rv[0].z, rv[0].w}, hi[4] = {rv[1].x, rv[1].y, rv[1].z, rv[1].w};
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -270,7 +277,7 @@ __global__ __launch_bounds__(256, 2) void ag_q8_prefill_kernel(pf_args a) {
   for (int t = t0; t < t1; ++t) {
     const int buf = (t - t0) & 1;
     const bool now = __builtin_amdgcn_readlane(w_id, t - w_first) >= 0;
-    const int ek = __builtin_amdgcn_readlane(w_ek, t - w_first), e_v = max(kQ8TileMinExp, __builtin_amdgcn_readlane(w_ev, t - w_first));
+    const int ek = __builtin_amdgcn_readlane(w_ek, t - w_first), e_v = max(kQ8PageMinExp, __builtin_amdgcn_readlane(w_ev, t - w_first));
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (what went to LDS by itself: the compiler does not know of it)
     __syncthreads();
     if (t + 1 < t1) {
@@ -298,7 +305,7 @@ __global__ __launch_bounds__(256, 2) void ag_q8_prefill_kernel(pf_args a) {
       }
       // s[x][i]: row 32 x + 8 (i / 4) + 4 h + i % 4 of the tile.  The state is kept relative to m, the largest score plus its tile's ev less
       // kQ8TopBits: a tile's weights are 2^(score + ev - m), at most 2^15, its values v 2^-ev, and its part of the row sum is 2^-ev the sum of
-      // its weights, as the second product takes them: what rounding them changes cancels.
+      // its weights, as the second product takes them: what rounding them changes cancels.  (`apart`: the sum of 2^(score - m).)
       const float f = q8_unscale(a.qscale, eq + ek), ev = (float)e_v;
       if (t >= meta.blocks && first + kQ8Block > see_all) {
         const int b = bound - first - 4 * h;
@@ -308,6 +315,8 @@ __global__ __launch_bounds__(256, 2) void ag_q8_prefill_kernel(pf_args a) {
           for (int i = 0; i < 16; ++i)
             if (32 * x + 8 * (i / 4) + i % 4 >= b) s[x][i] = -INFINITY;
       }
+      ev_top = max(ev_top, e_v);
+      const bool apart = e_v <= ev_top - kQ8Span;
       uint32_t p[2][8];
       float sum = 0.f;
       auto weigh = [&] {
@@ -325,7 +334,7 @@ __global__ __launch_bounds__(256, 2) void ag_q8_prefill_kernel(pf_args a) {
         sum = part[0] + part[1];
       };
       if (!fresh) weigh();
-      if (fresh || __any(!(sum <= 32768.f))) {  // no reference yet, or too far below: a new one, and the weights again
+      if (fresh || apart || __any(!(sum <= 32768.f))) {  // no reference yet, or too far below: a new one, and the weights again
         float mx = -INFINITY;
 #pragma unroll
         for (int x = 0; x < 2; ++x)
@@ -334,13 +343,20 @@ __global__ __launch_bounds__(256, 2) void ag_q8_prefill_kernel(pf_args a) {
         mx = fmaf(fmaxf(mx, other_half(mx)), f, ev - (float)kQ8TopBits);
         const float both = fmaxf(sum <= 32768.f ? 0.f : 1.f, other_half(sum <= 32768.f ? 0.f : 1.f));
         const float m_new = fresh || both > 0.f ? fmaxf(m, mx) : m;  // (a row's own reference alone: no row depends on its neighbours)
-        const float alpha = __builtin_amdgcn_exp2f(m - m_new);
-        l *= alpha;
+        const float alpha = half_way(m - m_new);
+        l = l * alpha * alpha;
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) o[dt] *= alpha;
+        for (int dt = 0; dt < DT; ++dt) o[dt] = o[dt] * alpha * alpha;
         m = m_new;
         fresh = false;
         weigh();
+        if (apart) {
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) l += __builtin_amdgcn_exp2f(fmaf(s[x][i], f, -m));
+          sum = 0.f;
+        }
       }
       l += ldexpf(sum, -e_v);
 #pragma unroll
@@ -378,16 +394,16 @@ __global__ __launch_bounds__(256, 2) void ag_q8_prefill_kernel(pf_args a) {
         s = (s + other_half(s)) * f;
         if (first + r < bound) {
           const float m_new = fmaxf(m, s < kQ8EmptyMax ? kQ8EmptyMax : s);
-          const float alpha = __builtin_amdgcn_exp2f(m - m_new), w = __builtin_amdgcn_exp2f(s - m_new);
+          const float alpha = half_way(m - m_new), w = __builtin_amdgcn_exp2f(s - m_new);
           m = m_new;
-          l = fmaf(l, alpha, h == 0 ? w : 0.f);
+          l = l * alpha * alpha + (h == 0 ? w : 0.f);
           // row r: step r / 16, half (r / 4) % 2, element 4 ((r / 8) % 2) + r % 4 of a column's piece
           const uint16_t *vr = tv + ((r >> 4) * 64 + ((r >> 2) & 1) * 32) * 8 + ((r >> 3) & 1) * 4 + (r & 3);
 #pragma unroll
           for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-              o[dt][i] = fmaf(o[dt][i], alpha, w * __uint_as_float((uint32_t)vr[(dt * 4 * 64 + 8 * (i / 4) + 4 * h + i % 4) * 8] << 16));
+              o[dt][i] = fmaf(o[dt][i] * alpha, alpha, w * __uint_as_float((uint32_t)vr[(dt * 4 * 64 + 8 * (i / 4) + 4 * h + i % 4) * 8] << 16));
         }
       }
     }
@@ -440,9 +456,9 @@ __global__ __launch_bounds__(256) void ag_q8_prefill_merge_kernel(pf_args a) {
     const float *f = from + (size_t)p * kRows * (D + 4);
     const float4 x = *reinterpret_cast<const float4 *>(f + d);
     const float2 ml = *reinterpret_cast<const float2 *>(f + D);
-    const float w = __builtin_amdgcn_exp2f(ml.x - M);
-    L = fmaf(w, ml.y, L);
-    o.x = fmaf(w, x.x, o.x); o.y = fmaf(w, x.y, o.y); o.z = fmaf(w, x.z, o.z); o.w = fmaf(w, x.w, o.w);
+    const float w = half_way(ml.x - M);
+    L = fmaf(w, ml.y * w, L);
+    o.x = fmaf(w, x.x * w, o.x); o.y = fmaf(w, x.y * w, o.y); o.z = fmaf(w, x.z * w, o.z); o.w = fmaf(w, x.w * w, o.w);
   }
   const float inv = 1.f / L;
   const int j = row / G, b = u / a.Hkv;

@@ -22,23 +22,25 @@ def _lib():
     ensure_built()
 
 
-def cache(g, B, H, D, longest, kind, bits):
-    """Units of 0 to `longest` rows over few pages that they share (each unit's last block has one of its own).  Half of the pages are
+def cache(g, B, H, D, longest, kind, bits, room=0):
+    """Units of 0 to `longest` rows over few pages that they share (the blocks that `room` more rows can fill have pages of their own).  Half of the pages are
     zeros: beside others 2^bits as large as usual; tiny: of the least scale, beside such;
     small: 2^-bits as large as usual, and preferred (a score higher by 512 / sqrt D); preferred: of zeros, and preferred."""
     U = B * H
     lens = torch.randint(0, longest + 1, (U,), generator=g).tolist()
     lens[U // 2] = longest
-    page = torch.randint(U, U + 16, (U, longest // 64 + 1), generator=g).int()
+    own = (room + 63) // 64 + 1
+    blocks, shared = longest // 64 + own, U * own
+    page = torch.randint(shared, shared + 16, (U, blocks), generator=g).int()
     for u in range(U):
-        page[u, lens[u] // 64] = u
-    c = R.Cache(B, H, D, U + 16, longest // 64 + 1, g, lens, page=page)
+        page[u, lens[u] // 64:lens[u] // 64 + own] = torch.arange(u * own, u * own + own)
+    c = R.Cache(B, H, D, shared + 16, blocks, g, lens, page=page)
     at = R.places(D)
     for x in c.tails:
         x[:, at[0][:, 0]] = 0.0
     half = torch.zeros(c.n_pages, dtype=torch.bool)
-    half[U:][torch.randperm(16, generator=g)[:8]] = True
-    for p in range(U, c.n_pages):
+    half[shared:][torch.randperm(16, generator=g)[:8]] = True
+    for p in range(shared, c.n_pages):
         keys = (c.codes[0][p] * c.scales[0][p]).clone()
         keys[at[0][:, 0]] = 64.0 if half[p] and kind in ("small", "preferred") else 0.0
         codes, c.scales[0][p] = R.eight_bits(keys)
@@ -82,3 +84,18 @@ def test_trees(B, H, G, D, L, longest, kind, bits):
     ag.ag_q8_tree_attn(ctx, q.to(DEV), k.to(DEV), v.to(DEV), f.to(DEV), parent.to(DEV), None, D ** -0.5, on_device(ref), out)
     ctx.poll_error()
     assert worst(out, T.attend(ref, q, k, v, f != 0, parent, D ** -0.5), ("tree", B, H, G, D, L, kind, bits)) <= BAR
+
+
+@pytest.mark.parametrize("own", [0, -40, 40])
+@pytest.mark.parametrize("kind,bits", SIZES)
+@pytest.mark.parametrize("B,H,G,D,L,longest", [(1, 4, 2, 128, 60, 2500), (33, 4, 1, 64, 130, 700), (1, 2, 4, 64, 80, 4000)])
+def test_turns(B, H, G, D, L, longest, kind, bits, own):
+    """own: the call's values are 2^own as large as usual, those of evicted tokens among them."""
+    g = gen(D + L + bits)
+    ref = cache(g, B, H, D, longest, kind, bits, L)
+    q, k, v = inputs(g, B, H * G, H, L, D, own)
+    f = flags_of(g, "rand", B, H, L)
+    ctx = ag.Context(0, ag.q8_workspace_bytes(B, L, H * G, H, D, ref.max_blocks))
+    out = torch.empty(q.shape, dtype=BF, device=DEV)
+    ag.ag_q8_prefill_attn(ctx, q.to(DEV), k.to(DEV), v.to(DEV), f.to(DEV), None, D ** -0.5, on_device(ref), out)
+    assert worst(out, R.attend(ref, q, k, v, f != 0, D ** -0.5), ("turn", B, H, G, D, L, kind, bits, own)) <= BAR
