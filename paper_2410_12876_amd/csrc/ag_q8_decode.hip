@@ -12,7 +12,7 @@
 //     11 bits of each, as the codes have 4; row sums add up the rounded weights.  The reference lies 2^-8 below the largest of the page that set it,
 //     so weights down to 2^-33 of that count; in the wave that has the tail the tail sets it, and those down to 2^-21 do.  (A weight in three
 //     bf16 parts in the columns that G < 16 leaves idle kept 24 bits: 32 sequences of 32 heads 533 us a 4 steps, now 443; output rows are off by 1.7e-3 of
-//     their size either way, which the store's rounding gives.)
+//     their size either way, which the store's rounding gives.)  Pages of far smaller values than others add to the row sum in 32 bits (kQ8Span).
 //   * The workgroup turns its queries and the new key together, into LDS: a lane's own row by itself took 64 lines a load.  The barrier
 //     after it waits for LDS alone, and the pages are asked for behind it: ahead of it they held up the small loads.
 //   * The tail is a page in bf16; the new token's row is put into it in registers, so that it is one row more.  The wave that has it also
@@ -96,6 +96,9 @@ __device__ __forceinline__ float kg_sum(float x) {
   const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
+// 2^(d / 2): what is to shrink by 2^d is multiplied by it twice (references of pages of very different sizes lie further apart than a factor
+// can be small).
+__device__ __forceinline__ float half_way(float d) { return __builtin_amdgcn_exp2f(0.5f * d); }
 // x as bf16 in the lower half of a word, what is left of it as bf16 in the upper one
 __device__ __forceinline__ float in_two(float x) {
   const float first = q8_lo(q8_pack2(x, 0.f));
@@ -119,7 +122,7 @@ template <int D, int G> struct wave_q8 {
 
   __device__ __forceinline__ void init(int lane_) {
     lane = lane_; g = lane >> 4; col = lane & 15; head = col % P; second = col >= P;
-    m = kQ8EmptyMax; l = 0.f; eq = 0;
+    m = kQ8EmptyMax; l = 0.f; eq = 0; ev_top = kQ8PageMinExp;
 #pragma unroll
     for (int f = 0; f < VF; ++f) o[f] = q8_f32x4{0.f, 0.f, 0.f, 0.f};
   }
@@ -151,10 +154,10 @@ template <int D, int G> struct wave_q8 {
   // A new reference for the scores (their tile's exponent included): everything so far shrinks to it.
   __device__ __forceinline__ void raise(float m_new) {
     if (__any(m_new != m)) {
-      const float alpha = __builtin_amdgcn_exp2f(m - m_new);
-      l *= alpha;
+      const float alpha = half_way(m - m_new);
+      l = l * alpha * alpha;
 #pragma unroll
-      for (int f = 0; f < VF; ++f) o[f] *= alpha;
+      for (int f = 0; f < VF; ++f) o[f] = o[f] * alpha * alpha;
       m = m_new;
     }
   }
@@ -166,11 +169,12 @@ template <int D, int G> struct wave_q8 {
     for (int f = 0; f < VF; ++f)
 #pragma unroll
       for (int r = 0; r < 4; ++r) top = fmaxf(top, fabsf(o[f][r]) < INFINITY ? fabsf(o[f][r]) : 0.f);
-    return (float)max(0, min(-kQ8TileMinExp, 127 + 120 - (int)(wave_max(__float_as_uint(top)) >> 23)));
+    return (float)max(0, min(-kQ8PageMinExp, 127 + 120 - (int)(wave_max(__float_as_uint(top)) >> 23)));
   }
 
   // A wave's pages: lane x holds the number and the exponents of its page x (of at most 64 at a time); two pages are in flight.
   int ids, ek_v, ev_v;
+  int ev_top;  // the largest exponent that the reference has been set with (a tail's has none: 0, which kHighBits leaves room for)
   // (The same registers hold a tail instead: as long as the two were told apart the compiler kept room for both.)
   q8_u32x4 buf[4 * KF];  // K of two pages, V of two pages; or a tail's K, V
   uint32_t nv[VF / 2];   // this lane's values of the new token, two a register
@@ -201,7 +205,7 @@ template <int D, int G> struct wave_q8 {
   }
   // Page x of n, which is in buffer B; that buffer's next one is asked for.  The state is kept relative to m, the largest score plus its page's
   // exponent ev of V less kQ8TopBits: a page's weights are 2^(score + ev - m) in f16, its values the codes 2^-kValueBits, its part of the row
-  // sum 2^-ev the sum of its weights (as the product takes them: what rounding them changes cancels).
+  // sum 2^-ev the sum of its weights (as the product takes them: what rounding them changes cancels; `apart`: the sum of 2^(score - m)).
   template <int B> __device__ __forceinline__ void one_page(const ag_q8_dev &c, int x, int n, float qscale, bool &fresh) {
     const bool more = x + 2 < n, now = __builtin_amdgcn_readlane(ids, x) >= 0;
     q8_f32x4 s[4];
@@ -216,7 +220,7 @@ template <int D, int G> struct wave_q8 {
     }
     if (more) load<B * KF>(c.k, x + 2);
     if (now) {
-      const int e = __builtin_amdgcn_readlane(ev_v, x), ev = max(kQ8TileMinExp, e + kValueBits);
+      const int e = __builtin_amdgcn_readlane(ev_v, x), ev = max(kQ8PageMinExp, e + kValueBits);
       const float f = q8_unscale(qscale, eq + __builtin_amdgcn_readlane(ek_v, x));
       float sum;
       uint32_t w[8];
@@ -241,15 +245,25 @@ template <int D, int G> struct wave_q8 {
         // The wave's first page.  The reference that a tail has left is a score without an exponent: where the values are small it is too high
         // for a page's weights in f16, and comes down (the state is in 32 bits).
         const float mx = largest();
-        raise(fmaxf(mx, __builtin_expect(__any(mx < m - kHighBits), 0) ? m - lower() : m));
+        float down = 0.f;
+        if (__builtin_expect(__any(mx < m - kHighBits), 0)) down = lower();
+        raise(fmaxf(mx, m - down));
+        ev_top -= (int)down;
       }
       fresh = false;
+      ev_top = max(ev_top, ev);
+      const bool apart = ev <= ev_top - kQ8Span;
       weigh();
       // no maximum in the common case: only where weights pass 2^15 is the reference moved (for that head alone)
-      if (__any(!(sum <= 32768.f))) {
+      if (apart || __any(!(sum <= 32768.f))) {
         const float m_new = fmaxf(m, largest());
         raise(kg_max(sum <= 32768.f ? 0.f : 1.f) > 0.f ? m_new : m);
         weigh();
+        if (apart) {
+#pragma unroll
+          for (int y = 0; y < 16; ++y) l += __builtin_amdgcn_exp2f(fmaf(s[y >> 2][y & 3], f, -m));
+          sum = 0.f;
+        }
       }
       l += ldexpf(sum, -ev);
       const float scale = q8_pow2(e - ev);
@@ -395,6 +409,7 @@ template <int D, int G> struct wave_q8 {
       if (lane == 0) a.c.k_scale[id] = q8_pow2(e);
     }
     raise(fmaxf(m, kg_max(mx)));
+    ev_top = 0;
     // A weight's first part is the first 16 bits of a number just below it, its second one what is left, rounded: both are positive
     // where the weight is not 0, so that an infinite value comes out with its sign.
     uint32_t w[8];
@@ -730,11 +745,11 @@ __global__ __launch_bounds__(64 * NW, 2) void ag_q8_decode_kernel(dec_args a) {
         for (int w = 0; w < NW; ++w) M = fmaxf(M, ms[w]);
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-          const float f = __builtin_amdgcn_exp2f(ms[w] - M);
+          const float f = half_way(ms[w] - M);
           const bool any = !(ls[w] == 0.f);  // (a wave without rows)
-          L = fmaf(f, ls[w], L);
-          A0 = any ? fmaf(f, o0[w], A0) : A0;
-          A1 = any ? fmaf(f, o1[w], A1) : A1;
+          L = fmaf(f, f * ls[w], L);
+          A0 = any ? fmaf(f, f * o0[w], A0) : A0;
+          A1 = any ? fmaf(f, f * o1[w], A1) : A1;
         }
         if (n_rec == 1) {
           store_out(gg, d, A0, A1, L);
@@ -765,16 +780,16 @@ __global__ __launch_bounds__(64 * NW, 2) void ag_q8_decode_kernel(dec_args a) {
             float M_new = M;
 #pragma unroll
             for (int j = 0; j < 8; ++j) M_new = fmaxf(M_new, ml[j].x);
-            const float keep = __builtin_amdgcn_exp2f(M - M_new);
+            const float keep = half_way(M - M_new);
             M = M_new;
-            L *= keep; A0 *= keep; A1 *= keep;
+            L = L * keep * keep; A0 = A0 * keep * keep; A1 = A1 * keep * keep;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
               if (k0 + j >= n_rec) break;
-              const float w = __builtin_amdgcn_exp2f(ml[j].x - M);
-              L = fmaf(w, ml[j].y, L);
-              A0 = fmaf(w, o[j].x, A0);
-              A1 = fmaf(w, o[j].y, A1);
+              const float w = half_way(ml[j].x - M);
+              L = fmaf(w, w * ml[j].y, L);
+              A0 = fmaf(w, w * o[j].x, A0);
+              A1 = fmaf(w, w * o[j].y, A1);
             }
           }
           store_out(gg, d, A0, A1, L);

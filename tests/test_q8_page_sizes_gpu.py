@@ -57,7 +57,8 @@ def cache(g, B, H, D, longest, kind, bits, room=0):
 
 def worst(got, want, what):
     got, want = got.double().cpu(), want.double()
-    e = ((got - want).pow(2).mean(-1) / want.pow(2).mean(-1)).sqrt()
+    off = ((got - want).abs() - 2.0 ** -126).clamp(min=0.0)  # smaller numbers are subnormal in bf16 (and in fp32): they have fewer bits, or are 0
+    e = (off.pow(2).mean(-1) / want.pow(2).mean(-1)).sqrt()
     print(*what, "row errors: mean %.2e, worst %.2e" % (e.mean().item(), e.max().item()), flush=True)
     return e.max().item() if bool(torch.isfinite(got).all()) else float("inf")
 
@@ -88,7 +89,7 @@ def test_trees(B, H, G, D, L, longest, kind, bits):
 
 @pytest.mark.parametrize("own", [0, -40, 40])
 @pytest.mark.parametrize("kind,bits", SIZES)
-@pytest.mark.parametrize("B,H,G,D,L,longest", [(1, 4, 2, 128, 60, 2500), (33, 4, 1, 64, 130, 700), (1, 2, 4, 64, 80, 4000)])
+@pytest.mark.parametrize("B,H,G,D,L,longest", [(1, 4, 2, 128, 60, 2500), (130, 4, 1, 64, 2, 500), (1, 2, 4, 64, 80, 4000)])
 def test_turns(B, H, G, D, L, longest, kind, bits, own):
     """own: the call's values are 2^own as large as usual, those of evicted tokens among them."""
     g = gen(D + L + bits)
@@ -99,3 +100,21 @@ def test_turns(B, H, G, D, L, longest, kind, bits, own):
     out = torch.empty(q.shape, dtype=BF, device=DEV)
     ag.ag_q8_prefill_attn(ctx, q.to(DEV), k.to(DEV), v.to(DEV), f.to(DEV), None, D ** -0.5, on_device(ref), out)
     assert worst(out, R.attend(ref, q, k, v, f != 0, D ** -0.5), ("turn", B, H, G, D, L, kind, bits, own)) <= BAR
+
+
+@pytest.mark.parametrize("own", [0, -40, 40])
+@pytest.mark.parametrize("kind,bits", SIZES)
+@pytest.mark.parametrize("B,H,G,D,longest", [(1, 4, 2, 128, 6000), (40, 8, 1, 64, 300), (40, 8, 4, 128, 900), (2, 2, 8, 64, 9000)])
+def test_steps(B, H, G, D, longest, kind, bits, own):
+    """own: the tails' values and the new token's are 2^own as large as usual."""
+    g = gen(D + longest + bits)
+    ref = cache(g, B, H, D, longest, kind, bits)
+    ref.tails[1] *= 2.0 ** own
+    q, k, v = inputs(g, B, H * G, H, 1, D, own)
+    ctx = ag.Context(0, ag.q8_workspace_bytes(B, 1, H * G, H, D, ref.max_blocks))
+    out = torch.empty(B, H * G, D, dtype=BF, device=DEV)
+    one = lambda x: x[:, :, 0].contiguous().to(DEV)  # noqa: E731
+    ag.ag_q8_decode_attn(ctx, one(q), one(k), one(v), torch.zeros(B, H, dtype=torch.uint8, device=DEV), None, D ** -0.5, on_device(ref), out)
+    ctx.poll_error()
+    want = R.attend(ref, q, k, v, torch.zeros(B, H, 1, dtype=torch.bool), D ** -0.5)[:, :, 0]
+    assert worst(out, want, ("step", B, H, G, D, kind, bits, own)) <= BAR
