@@ -37,7 +37,7 @@ struct q8_tile_info {
   bool odd;
 };
 constexpr int kQ8TileTop = 14;      // a tile's largest number lies in [2^14, 2^15) ...
-constexpr int kQ8TileMinExp = -60;  // ... unless that took a smaller exponent than this (sums of 2^-ev stay in range)
+constexpr int kQ8TileMinExp = -60;  // ... unless that took a smaller exponent than this (queries, keys; values: kQ8PageMinExp)
 constexpr int kQ8TileSpan = 16;
 // Weights are f16 relative to a reference that lies this many bits below the largest one when it is set: those down to 2^-22 of it
 // keep their 11 bits, those down to 2^-33 some, and a long cache's many small ones are not lost.
@@ -47,7 +47,7 @@ constexpr int kQ8TopBits = 8;
 // its values hardly count beside the others', but its rows count in the row sum.  Where ev lies kQ8Span or more below the largest of those that
 // can have set the reference, the row sum takes the page's weights in 32 bits, 2^(score - m), apart from the products.
 constexpr int kQ8Span = 4;
-constexpr int kQ8PageMinExp = -90;  // least ev: row sums of 2^18 rows stay in range, and codes (2^-9 at least) of a block of scale 2^-100 exact in f16
+constexpr int kQ8PageMinExp = -90;  // least ev, tiles' too: row sums of 2^18 rows stay in range, and codes (2^-9 at least) of a block of scale 2^-100 exact in f16
 
 // What ag_q8_fill_kernel leaves for the attention of the same call: the unit's cache as it stood before it.
 struct ag_q8_meta {

@@ -370,7 +370,7 @@ __global__ __launch_bounds__(4 * D, 4) void ag_q8_fill_kernel(fill_args a) {
       auto binade = [](uint32_t top) { return max((int)(top >> 7), 1) - 127; };
       const bool row_by_row = odd || (block_k && binade(of.least[0]) + kQ8TileSpan < binade(block_k)) ||
                               (block_v && binade(of.least[1]) + kQ8TileSpan < binade(block_v));
-      const int ek = max(kQ8TileMinExp, binade(block_k) - kQ8TileTop), ev = max(kQ8TileMinExp, binade(block_v) - kQ8TileTop);
+      const int ek = max(kQ8TileMinExp, binade(block_k) - kQ8TileTop), ev = max(kQ8PageMinExp, binade(block_v) - kQ8TileTop);
       const float ik = q8_pow2(-ek), iv = q8_pow2(-ev);
       uint16_t *tk = a.tiles + ((size_t)u * a.n_blk + j) * 2 * kQ8Block * D, *tv = tk + kQ8Block * D;
 #pragma unroll

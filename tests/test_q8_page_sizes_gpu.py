@@ -118,3 +118,17 @@ def test_steps(B, H, G, D, longest, kind, bits, own):
     ctx.poll_error()
     want = R.attend(ref, q, k, v, torch.zeros(B, H, 1, dtype=torch.bool), D ** -0.5)[:, :, 0]
     assert worst(out, want, ("step", B, H, G, D, kind, bits, own)) <= BAR
+
+
+@pytest.mark.parametrize("bits", [-40, -76, -90, -100])
+@pytest.mark.parametrize("D,lens", [(128, [0, 0]), (64, [0, 30])])
+def test_turns_of_small_values(D, lens, bits):
+    """Nothing but the call's own values (and a tail's), 2^bits as large as usual."""
+    g, L, H = gen(D - bits), 90, 2
+    ref = R.Cache(1, H, D, H * 3, 3, g, lens)
+    ref.tails[1] *= 2.0 ** bits
+    q, k, v, f = some(g, 1, 2 * H, L, D), some(g, 1, H, L, D), (some(g, 1, H, L, D).float() * 2.0 ** bits).to(BF), flags_of(g, "rand", 1, H, L)
+    ctx = ag.Context(0, ag.q8_workspace_bytes(1, L, 2 * H, H, D, ref.max_blocks))
+    out = torch.empty(q.shape, dtype=BF, device=DEV)
+    ag.ag_q8_prefill_attn(ctx, q.to(DEV), k.to(DEV), v.to(DEV), f.to(DEV), None, D ** -0.5, on_device(ref), out)
+    assert worst(out, R.attend(ref, q, k, v, f != 0, D ** -0.5), ("turn", D, lens, bits)) <= BAR
