@@ -28,6 +28,11 @@ template <typename T> __device__ __forceinline__ uint4 pack(const float *f) {
   return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
 }
 
+// Which vector of q (of k, from head Hq on) head j of token t of sequence b is: 64 bits, 2^31 of 16 values are 64 GiB.
+__device__ __forceinline__ size_t vector_at(int b, int t, int j, int Hq, int Hkv, int L) {
+  return (j < Hq ? (size_t)b * Hq + j : (size_t)b * Hkv + (j - Hq)) * L + t;
+}
+
 // grid (chunks of 256 (token, piece) pairs, groups of `heads` heads).  q and q_out (k and k_out) may be the same memory.
 template <typename T>
 __global__ __launch_bounds__(256) void ag_rotate_kernel(const T *q, const T *k, T *q_out, T *k_out, int tokens, int Hq, int Hkv, int L,
@@ -58,7 +63,7 @@ __global__ __launch_bounds__(256) void ag_rotate_kernel(const T *q, const T *k, 
   const int h0 = blockIdx.y * heads, h1 = min(h0 + heads, Hq + Hkv);
   for (int h = h0; h < h1; h += kHeadsAtOnce) {
     uint4 lo[kHeadsAtOnce], hi[kHeadsAtOnce];
-    auto place = [&](int j) { return (((size_t)(j < Hq ? b * Hq + j : b * Hkv + j - Hq)) * L + t) * D + i; };
+    auto place = [&](int j) { return vector_at(b, t, j, Hq, Hkv, L) * D + i; };
 #pragma unroll
     for (int x = 0; x < kHeadsAtOnce; ++x) {
       const int j = min(h + x, h1 - 1);
@@ -124,7 +129,7 @@ __global__ __launch_bounds__(256) void ag_norm_rotate_kernel(const T *q, const T
   const int h0 = blockIdx.y * heads, h1 = min(h0 + heads, Hq + Hkv);
   for (int h = h0; h < h1; h += kHeadsAtOnce) {
     uint4 lo[kHeadsAtOnce], hi[kHeadsAtOnce];
-    auto place = [&](int j) { return (((size_t)(j < Hq ? b * Hq + j : b * Hkv + j - Hq)) * L + t) * D + at_i; };
+    auto place = [&](int j) { return vector_at(b, t, j, Hq, Hkv, L) * D + at_i; };
 #pragma unroll
     for (int x = 0; x < kHeadsAtOnce; ++x) {
       const int j = min(h + x, h1 - 1);
