@@ -299,7 +299,8 @@ typedef struct {
 /*
  * Queries and keys turned by their positions, in one launch: q, q_out [B, Hq, L, D], k, k_out [B, Hkv, L, D] in `dtype`;
  * q_out may be q, k_out may be k.  k and k_out may be NULL (Hkv is then ignored).  bf16 or fp32, D a multiple of 16 and at most
- * 512; all tensors 16-byte aligned.  Needs no workspace.
+ * 512; all tensors 16-byte aligned.  Needs no workspace.  At most 2^32 - 256 threads, of which a token has as many as D / 2 values have pieces
+ * of 16 bytes.
  */
 ag_status ag_rotate(ag_ctx *ctx, void *hip_stream, const void *q, const void *k, ag_dtype dtype, int B, int Hq, int Hkv, int L,
                     int D, const ag_rope *rope, void *q_out, void *k_out);

@@ -101,7 +101,9 @@ ag_status ag_rotate(ag_ctx *ctx, void *hip_stream, const void *q, const void *k,
   AG_REQUIRE(B > 0 && Hq > 0 && L > 0 && D > 0 && (!k || Hkv > 0), AG_EINVAL, "ag_rotate: sizes must be positive");
   AG_REQUIRE(dtype == AG_F32 || dtype == AG_BF16, AG_EINVAL, "ag_rotate: unknown dtype %d", (int)dtype);
   AG_REQUIRE(D % 16 == 0 && D <= 512, AG_EUNSUPPORTED, "ag_rotate: D = %d (a multiple of 16, at most 512)", D);
-  AG_REQUIRE(L <= kMaxL && (int64_t)B * L < (1ll << 31) && (int64_t)Hq + Hkv <= 65535, AG_EUNSUPPORTED, "ag_rotate: problem too large");
+  const int pieces = D / 2 / (dtype == AG_BF16 ? 8 : 4);  // (a token's threads; a launch has fewer than 2^32)
+  AG_REQUIRE(L <= kMaxL && (int64_t)B * L < (1ll << 31) && (int64_t)B * L * pieces <= (1ll << 32) - 256 && (int64_t)Hq + Hkv <= 65535, AG_EUNSUPPORTED,
+             "ag_rotate: problem too large");
   AG_REQUIRE(aligned({q, k, q_out, k_out}), AG_EINVAL, "ag_rotate: tensors must be 16-byte aligned");
   ag_rope_dev r;
   ag_status st = check_rope(ctx, "ag_rotate", rope, D, (int64_t)B * L, &r, false);
