@@ -308,8 +308,8 @@ ag_status ag_rotate(ag_ctx *ctx, void *hip_stream, const void *q, const void *k,
 /*
  * Queries and keys normalised head by head and then turned by their positions, in one launch: every vector x of D values of q (k) becomes
  *   n_i = (x_i r) w_i,   r = 1 / sqrt(mean_i x_i^2 + eps),   w = q_weight (k_weight)
- * and n is turned as ag_rotate turns it; all in 32 bits, products and sums rounded one by one, one rounding to `dtype` at the end.  rope = NULL: n
- * itself.  q_weight, k_weight [D] in `dtype`; eps >= 2^-100; k, k_out and k_weight may be NULL together (Hkv is then ignored).  Layouts, types,
+ * and n is turned as ag_rotate turns it; all in 32 bits, products and the turn's sums rounded one by one (the sum of squares by fused
+ * multiply-adds), one rounding to `dtype` at the end.  rope = NULL: n itself.  q_weight, k_weight [D] in `dtype`; eps >= 2^-100; k, k_out and k_weight may be NULL together (Hkv is then ignored).  Layouts, types,
  * D and alignment (the weights' too) as for ag_rotate; q_out may be q, k_out may be k.  Needs no workspace.  At most 2^32 - 256 threads, of which a
  * token has as many as D / 2 values have pieces of 16 bytes, rounded up to a power of two.
  */

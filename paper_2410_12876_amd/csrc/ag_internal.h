@@ -30,7 +30,10 @@ struct ag_ctx {
   char *ws;         // device workspace
   size_t ws_bytes;
   int32_t *d_err;   // sticky device error word (bit 0: cache capacity overflow, bit 1: position outside a rotation table, bit 2: node of a tree)
-  int32_t *decode_tickets;  // [kDecodeMaxUnits + kDecodeArriveInts] arrival counters of a decode step: zero between launches
+  // [kDecodeMaxUnits + kDecodeArriveInts] arrival counters: of a decode step's pieces (over either cache) and workgroups, of the units of an
+  // append to the paged cache, of a tree's pieces (by their record), of the workgroups that move a small pool.  Every launch finds them zero and
+  // leaves them zero, and no two of them overlap: a context's work is on one stream at a time.
+  int32_t *decode_tickets;
   int32_t *prefill_tickets; // [kPrefillTickets] arrival counters of a prefill launch without a flag scan: zero between launches
   char *static_scratch;   // this device's copy of the library's static scratch array (ag_decode_attn_static)
   bool timing;

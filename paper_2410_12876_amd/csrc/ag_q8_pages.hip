@@ -148,8 +148,9 @@ __global__ __launch_bounds__(kThreads) void ag_q8_reserve_kernel(ag_q8_dev c, in
   if (out) atomicOr(err, 1);
 }
 
-// The same in one launch, by one workgroup, for a small pool, units of which a thread takes one each, and few blocks: 500 pages and 32 units 2.5 us
-// (in two launches 4.6), 8000 pages and 1024 units 4.3 (5.5); 24800 pages 14 (8), 256 units that want 16 blocks each 9.1 (5.2).
+// The same in one launch, by one workgroup, for a small pool, units of which a thread takes one each, and few blocks: 500 pages and 32 units 3.1 us
+// (in two launches 2.2 + 3.8), 8000 pages and 1024 units 7.2 (3.8 + 4.3, and 2 to 3 between them).  More pages or blocks are better off in two: 24800
+// pages took one workgroup 14 us (4.5 + 4.7), 256 units that want 16 blocks each 9.1 (5.2).
 constexpr int kSmallPages = 8 * kListThreads, kSmallBlocks = 4;
 __global__ __launch_bounds__(kListThreads) void ag_q8_reserve_small_kernel(ag_q8_dev c, int32_t *page, int32_t *ref, int U, int rows, int32_t *err) {
   constexpr int WAVES = kListThreads / 64, N = kSmallPages / kListThreads;

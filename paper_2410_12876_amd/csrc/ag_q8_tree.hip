@@ -4,7 +4,8 @@
 // Query rows of a unit are its nodes' heads, r = t G + head; a wave owns 32 of them, a lane one column: S^T = K q^T, O^T = V^T p^T on
 // v_mfma_f32_32x32x16.  Bound by the pages' bytes while a unit has few rows (32 rows: 0.65 us a page of 16 KiB a CU, 6.5 TB/s; 64: 0.83 us, 5.05 TB/s),
 // beyond by the matrix instructions and the conversions and weights between them (128: 1.30 us, 0.82 PFLOP/s).  A short call is a chain of
-// round trips: 12 nodes over 777 rows 14.8 us; 16 x 31 nodes over 4096 rows 40.5 us, of which the pages take 23, the start 8 and the meetings 7.
+// round trips: 12 nodes over 777 rows 14.8 us (D = 64: 11.3); 16 x 31 nodes over 4096 rows 40.5 us (28.7), of which the pages take 23, the start 8 and the
+// meetings 7.  More units than CUs are rounds of that chain: 512 units of 8 nodes over 400 rows 34 us, 1024 64 (over 1600 rows 89).
 //   * A page goes from memory into the registers as it lies, and there, made f16 (exact, two values an instruction), into the product: its
 //     16-byte pieces are 16 columns of a row (4 x 4 rows of a column) for either half of the wave, in the order in which the query's
 //     (the weights') registers are.  No LDS, no barrier between pages; a page's registers are asked for again as soon as they are used up.
@@ -908,6 +909,8 @@ int tiles_of(int rows, int groups) { return (rows + 32 * groups - 1) / (32 * gro
 // rows, and less to add up.  So as few as leave a tile for every CU at most, while there are few pages to go through: up to 16 a CU one group (4 x 31
 // nodes over 1500 rows, G = 4, 8 heads: 20.3 us with one, 20.8 with two, 24 with four; over 3000 29 / 26 / 28), up to 96 two (over 9000 57 / 39 / 43; 4 x 64
 // nodes over 13000 54 with two, 51 with four).  With more tiles than CUs the rest would wait: 32 x 16 nodes over 100 rows 29 / 16.
+// The lengths are on the device, so the pages are those that the table has columns for.  A table made for much longer units costs what four groups
+// cost short ones: with 500 columns more 4 x 31 nodes over 1500 rows 24 us in place of 19, 64 over 777 22 in place of 17, 12 over 777 17 in place of 15.
 int row_groups(int num_cu, int units, int rows, int max_blocks) {
   const int n = tiles_of(rows, 1);
   const int64_t pages = (int64_t)units * n * max_blocks;
