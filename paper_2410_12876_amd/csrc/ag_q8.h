@@ -45,7 +45,8 @@ constexpr int kQ8TopBits = 8;
 // A page's values are made f16 by an exponent ev of their own (all of a page's codes are exact then), and what a weight is kept relative to holds
 // the score and ev: 2^(score + ev - m).  So a page of values far smaller than others' (of zeros: the least scale) has weights too small for f16:
 // its values hardly count beside the others', but its rows count in the row sum.  Where ev lies kQ8Span or more below the largest of those that
-// can have set the reference, the row sum takes the page's weights in 32 bits, 2^(score - m), apart from the products.
+// can have set the reference, the row sum takes the page's weights in 32 bits, 2^(score - m), apart from the products.  (Not for all: a tree of 16 x 31
+// nodes half of whose pages are zeros takes 49.5 us, with none 39.7.  Above that, weights down to 2^-18 of the largest keep their 11 bits.)
 constexpr int kQ8Span = 4;
 constexpr int kQ8PageMinExp = -90;  // least ev, tiles' too: row sums of 2^18 rows stay in range, and codes (2^-9 at least) of a block of scale 2^-100 exact in f16
 
